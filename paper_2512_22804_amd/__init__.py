@@ -1,7 +1,8 @@
 """MI355X-native MoR (Mixture of Representations) analyse-select-quantize path.
 
 ``binding``   ctypes front end of the C-ABI library ``libmor.so`` (HIP kernels for gfx950);
+``mx``        the same for microscaled 4-bit operands, their products and tokens sorted by expert (``mor_mx.h``);
 ``build``     compiles that library in-tree with hipcc;
 ``workloads`` seeded synthetic BF16 operands (no method arithmetic).
 """
-__all__ = ["binding", "build", "workloads"]
+__all__ = ["binding", "build", "mx", "workloads"]

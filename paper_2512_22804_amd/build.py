@@ -9,12 +9,15 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmor.so")
-SOURCES = ["mor_kernels.hip", "mor_partitions.hip", "mor_api.hip"]
-HEADERS = ["mor_device.h", "mor_launch.h", "mor_stream.h", "mor_sub1x128.h", "mor_team.h", os.path.join("..", "..", "include", "mor.h")]
+SOURCES = ["mor_kernels.hip", "mor_partitions.hip", "mor_api.hip", "mx_quantize.hip", "mx_product.hip", "mx_experts.hip", "mx_api.hip"]
+HEADERS = ["mor_device.h", "mor_launch.h", "mor_stream.h", "mor_sub1x128.h", "mor_team.h", "mx_device.h", "mx_launch.h",
+           os.path.join("..", "..", "include", "mor.h"), os.path.join("..", "..", "include", "mor_mx.h")]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off", "-fno-fast-math",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wall", "-Wno-unused-command-line-argument"]
 
@@ -25,16 +28,23 @@ def build(force: bool = True, verbose: bool = False) -> str:
     if not force and os.path.exists(LIB) and all(os.path.getmtime(LIB) >= os.path.getmtime(d) for d in deps):
         return LIB
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    cmd = [hipcc, *FLAGS, "-shared", "-o", LIB, *srcs]
-    if verbose:
-        print(" ".join(cmd))
-    res = subprocess.run(cmd, capture_output=True, text=True)
     noise = ("packed-fp32-ops", "is not a recognized feature")
-    err = "\n".join(l for l in res.stderr.splitlines() if not any(n in l for n in noise))
-    if res.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + res.stderr)
-    if verbose and err.strip():
-        print(err, file=sys.stderr)
+
+    def run(cmd):
+        if verbose:
+            print(" ".join(cmd))
+        res = subprocess.run(cmd, capture_output=True, text=True)
+        if res.returncode != 0:
+            raise RuntimeError("hipcc failed:\n" + res.stderr)
+        err = "\n".join(l for l in res.stderr.splitlines() if not any(n in l for n in noise))
+        if verbose and err.strip():
+            print(err, file=sys.stderr)
+
+    with tempfile.TemporaryDirectory() as tmp:
+        objs = [os.path.join(tmp, os.path.basename(s) + ".o") for s in srcs]
+        with ThreadPoolExecutor(min(len(srcs), os.cpu_count() or 1)) as pool:
+            list(pool.map(lambda so: run([hipcc, *FLAGS, "-c", "-o", so[1], so[0]]), zip(srcs, objs)))
+        run([hipcc, *FLAGS, "-shared", "-o", LIB, *objs])
     return LIB
 
 

@@ -1,0 +1,116 @@
+// Device-side building blocks of the microscaled 4-bit operands (gfx950 only).
+//
+// Arithmetic contract (bit-identical codes and scales):
+//   amax   = largest magnitude of the block, compared as bit patterns, so that an infinity or a NaN wins;
+//   byte   = biased exponent of the scale 2^e: from the binary32 exponent of amax (scale_byte below);
+//   |x| 2^-e is exact in binary32 unless it is far below the grid's smallest step, where it rounds to code 0;
+//   code   = nearest grid value, ties to the even code (hardware conversion), or the stochastic rule of mor_mx.h.
+#pragma once
+#include "mor_device.h"
+
+namespace mor {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+constexpr uint32_t kMxNan = 255u;
+
+// E8M0 byte of a block from the binary32 bits of its amax.  For a normal amax of biased exponent E the floor rule's exponent is
+// E - 127 - 2, stored with a bias of 127; subnormals and the smallest normals clamp to 2^-127 (byte 0).
+__device__ __forceinline__ uint32_t mx_scale_byte(uint32_t amax_bits, bool ceil_rule) {
+    if (amax_bits == 0u) return 127u;
+    if (amax_bits >= 0x7F800000u) return kMxNan;
+    int e = (int)(amax_bits >> 23) - 2;
+    if (ceil_rule && (amax_bits & 0x7FFFFFu) > 0x400000u) ++e;      // amax > 1.5 * 2^(e+2) = 6 * 2^e
+    return (uint32_t)max(e, 0);
+}
+// 2^(byte - 127) and its inverse as binary32; byte 0 is the subnormal 2^-127.
+__device__ __forceinline__ float mx_scale_value(uint32_t byte) { return __uint_as_float(byte ? byte << 23 : 0x00400000u); }
+__device__ __forceinline__ float mx_scale_inverse(uint32_t byte) { return __uint_as_float((254u - min(byte, 253u)) << 23); }
+
+// Philox 4 x 32 (J. Salmon, M. Moraes, R. Dror, D. Shaw: "Parallel random numbers: as easy as 1, 2, 3", 2011) with seven
+// rounds, the fewest for which the authors report that every statistical test passes; ten cost 1.4 times as much.
+__device__ __forceinline__ u32x4 philox(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3, uint32_t k0, uint32_t k1) {
+#pragma unroll
+    for (int i = 0; i < 7; ++i) {
+        const uint64_t p0 = (uint64_t)c0 * 0xD2511F53u, p1 = (uint64_t)c2 * 0xCD9E8D57u;
+        c0 = (uint32_t)(p1 >> 32) ^ c1 ^ k0;
+        c1 = (uint32_t)p1;
+        c2 = (uint32_t)(p0 >> 32) ^ c3 ^ k1;
+        c3 = (uint32_t)p0;
+        k0 += 0x9E3779B9u;
+        k1 += 0xBB67AE85u;
+    }
+    return u32x4{c0, c1, c2, c3};
+}
+
+// Stochastic code of one value: v = element in binary32, inv = 2^-e, r = 16 random bits.
+__device__ __forceinline__ uint32_t mx_code_stochastic(float v, float inv, uint32_t r) {
+    const float y = __builtin_fabsf(v) * inv;
+    const float per_step = y < 2.0f ? 2.0f : (y < 4.0f ? 1.0f : 0.5f);
+    const uint32_t first = y < 2.0f ? 0u : (y < 4.0f ? 2u : 4u);    // code minus multiple of the step
+    const uint32_t code = min((uint32_t)(y * per_step + (float)r * 0x1p-16f) + first, 7u);
+    return code | ((__float_as_uint(v) >> 31) << 3);
+}
+
+__device__ __forceinline__ bf16x2 bf16_pair(uint32_t word) { return __builtin_bit_cast(bf16x2, word); }
+
+// Eight elements to eight codes (element 0 in the lowest nibble).  Values as packed BF16 pairs or in binary32.
+__device__ __forceinline__ uint32_t mx_codes8_nearest(const u32x4& v, uint32_t byte) {
+    const float s = __uint_as_float(byte << 23);                    // the conversion reads the exponent field alone
+    uint32_t c = 0;
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, bf16_pair(v[0]), s, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, bf16_pair(v[1]), s, 1);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, bf16_pair(v[2]), s, 2);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, bf16_pair(v[3]), s, 3);
+    return byte == kMxNan ? 0u : c;
+}
+__device__ __forceinline__ uint32_t mx_codes8_nearest(const float (&v)[8], uint32_t byte) {
+    const float s = __uint_as_float(byte << 23);
+    uint32_t c = 0;
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[0], v[1], s, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[2], v[3], s, 1);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[4], v[5], s, 2);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[6], v[7], s, 3);
+    return byte == kMxNan ? 0u : c;
+}
+__device__ __forceinline__ uint32_t mx_codes8_stochastic(const float (&v)[8], uint32_t byte, const u32x4& random) {
+    const float inv = mx_scale_inverse(byte);
+    uint32_t c = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        c |= mx_code_stochastic(v[2 * j], inv, random[j] & 0xFFFFu) << (8 * j);
+        c |= mx_code_stochastic(v[2 * j + 1], inv, random[j] >> 16) << (8 * j + 4);
+    }
+    return byte == kMxNan ? 0u : c;
+}
+__device__ __forceinline__ void widen8(const u32x4& raw, float (&v)[8]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        v[2 * j] = __uint_as_float(raw[j] << 16);
+        v[2 * j + 1] = __uint_as_float(raw[j] & 0xFFFF0000u);
+    }
+}
+
+
+// Eight elements of a BF16 row from column c on; the last ones of a row may be missing and read as zeros.  Rows may start at any
+// element: the wide accesses need no more than the elements' own alignment.
+__device__ __forceinline__ u32x4 load8(const uint16_t* row, int64_t c, int64_t cols) {
+    u32x4 v{0u, 0u, 0u, 0u};
+    if (c + 8 <= cols) { __builtin_memcpy(&v, row + c, 16); return v; }
+    for (int j = 0; j < 8; ++j)
+        if (c + j < cols) v[j >> 1] |= (uint32_t)row[c + j] << (16 * (j & 1));
+    return v;
+}
+__device__ __forceinline__ void store8(uint16_t* row, int64_t c, int64_t cols, const u32x4& v) {
+    if (c + 8 <= cols) { __builtin_memcpy(row + c, &v, 16); return; }
+    for (int j = 0; j < 8; ++j)
+        if (c + j < cols) row[c + j] = (uint16_t)(v[j >> 1] >> (16 * (j & 1)));
+}
+// Nearest BF16 value, ties to even; a NaN becomes the quiet NaN of its sign.
+__device__ __forceinline__ uint32_t bf16_of(float v) {
+    const uint32_t u = __float_as_uint(v);
+    if ((u & 0x7FFFFFFFu) > 0x7F800000u) return 0x7FC0u | ((u >> 16) & 0x8000u);
+    return (u + 0x7FFFu + ((u >> 16) & 1u)) >> 16;
+}
+
+}  // namespace mor

@@ -1,0 +1,259 @@
+// Tokens sorted by expert and back: the order, rows gathered into it, weighted sums out of it, and the gradients.
+#include <algorithm>
+
+#include "mx_device.h"
+#include "mx_launch.h"
+
+namespace mor {
+namespace {
+
+constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
+constexpr int kMaxExperts = 1024;       // one lane each
+constexpr int kSortChunk = 4096;        // choices of a workgroup
+
+__device__ __forceinline__ uint32_t expert_of(const int32_t* ids, int64_t i, int64_t n, uint32_t experts) {
+    const uint32_t e = i < n ? (uint32_t)ids[i] : experts;
+    return e < experts ? e : experts;   // dropped
+}
+
+// Choices of each expert in each chunk; integer sums, so their order does not matter.
+__global__ __launch_bounds__(kSortThreads) void k_expert_count(const int32_t* ids, int64_t choices, uint32_t experts, uint32_t* counts) {
+    __shared__ uint32_t hist[kMaxExperts + 1];
+    for (uint32_t e = threadIdx.x; e <= experts; e += kSortThreads) hist[e] = 0u;
+    __syncthreads();
+    const int64_t i0 = (int64_t)blockIdx.x * kSortChunk;
+#pragma unroll
+    for (int j = 0; j < kSortChunk / kSortThreads; ++j) {
+        const uint32_t e = expert_of(ids, i0 + j * kSortThreads + threadIdx.x, choices, experts);
+        if (e < experts) atomicAdd(&hist[e], 1u);
+    }
+    __syncthreads();
+    for (uint32_t e = threadIdx.x; e < experts; e += kSortThreads) counts[(int64_t)blockIdx.x * experts + e] = hist[e];
+}
+
+// Sum over the 1024 lanes before this one (an exclusive scan); `wave_sums` [kSortWaves].
+__device__ __forceinline__ uint32_t scan_before(uint32_t v, uint32_t* wave_sums) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t upto = v;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t other = (uint32_t)__shfl_up((int)upto, d);
+        if (lane >= d) upto += other;
+    }
+    if (lane == 63) wave_sums[wave] = upto;
+    __syncthreads();
+    uint32_t before = 0u;
+    for (int w = 0; w < wave; ++w) before += wave_sums[w];
+    return before + upto - v;
+}
+
+// The places of a chunk's choices.  LONE: one chunk in all, which is counted here; else the counts of every chunk are read.
+// Lane e holds expert e's sums.  Within 64 choices the lanes of one expert find each other by ballots over the bits of its number,
+// so a choice's rank needs no atomic and the order is the choices' own.
+template <bool LONE>
+__global__ __launch_bounds__(kSortThreads) void k_expert_place(const int32_t* ids, int64_t choices, const uint32_t* counts, MxOrder o) {
+    __shared__ uint32_t next[kMaxExperts + 1];              // slot of the expert's next choice
+    __shared__ uint32_t wave_sums[kSortWaves];
+    __shared__ uint8_t in_wave[kSortWaves][kMaxExperts];    // choices of the expert among a wave's 64
+    const uint32_t experts = (uint32_t)o.n_experts, e = threadIdx.x, chunks = gridDim.x;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t total = 0u, earlier = 0u;
+    if (LONE) {
+        if (e <= experts) next[e] = 0u;
+        if (e == 0) next[experts] = 0u;
+        __syncthreads();
+        for (int64_t i = threadIdx.x; i < choices; i += kSortThreads) {
+            const uint32_t id = expert_of(ids, i, choices, experts);
+            if (id < experts) atomicAdd(&next[id], 1u);
+        }
+        __syncthreads();
+        if (e < experts) total = next[e];
+        __syncthreads();
+    } else if (e < experts) {
+        for (uint32_t c = 0; c < chunks; ++c) {
+            const uint32_t n = counts[(int64_t)c * experts + e];
+            if (c < blockIdx.x) earlier += n;
+            total += n;
+        }
+    }
+    const uint32_t padded = (total + o.align - 1) / o.align * o.align;
+    const uint32_t start = scan_before(padded, wave_sums);
+    if (e < experts) next[e] = start + earlier;
+    if (blockIdx.x == 0) {
+        if (e < experts) o.offsets[e] = (int32_t)start;
+        if (e == experts - 1) o.offsets[experts] = (int32_t)(start + padded);
+    }
+    // empty slots: those of the experts are shared out lane by lane, those behind the last one over all workgroups
+    if (e < experts && e % chunks == blockIdx.x)
+        for (uint32_t s = start + total; s < start + padded; ++s)
+            if (s < (uint32_t)o.capacity) o.src[s] = -1;
+    __shared__ uint32_t end;
+    if (e == experts - 1) end = start + padded;
+    __syncthreads();
+    for (int64_t s = (int64_t)end + blockIdx.x * kSortThreads + threadIdx.x; s < o.capacity; s += (int64_t)chunks * kSortThreads) o.src[s] = -1;
+
+    const int64_t i0 = (int64_t)blockIdx.x * kSortChunk;
+    for (int j = 0; j < kSortChunk / kSortThreads; ++j) {
+        const int64_t i = i0 + j * kSortThreads + threadIdx.x;
+        if (i0 + j * kSortThreads >= choices) break;
+        for (uint32_t q = threadIdx.x; q < kSortWaves * kMaxExperts / 4; q += kSortThreads) reinterpret_cast<uint32_t*>(in_wave)[q] = 0u;
+        __syncthreads();
+        const uint32_t id = expert_of(ids, i, choices, experts);
+        uint64_t same = __ballot(id < experts);
+        for (uint32_t bit = 1u; bit < experts; bit <<= 1) {
+            const uint64_t set = __ballot((id & bit) != 0u);
+            same &= (id & bit) ? set : ~set;
+        }
+        const uint32_t rank = __popcll(same & ((1ull << lane) - 1ull));
+        if (id < experts && rank == 0) in_wave[wave][id] = (uint8_t)__popcll(same);
+        __syncthreads();
+        if (id < experts) {
+            uint32_t slot = next[id] + rank;
+            for (int w = 0; w < wave; ++w) slot += in_wave[w][id];
+            o.slot_of[i] = (int32_t)slot;
+            if (slot < (uint32_t)o.capacity) o.src[slot] = (int32_t)i;
+        } else if (i < choices) o.slot_of[i] = -1;
+        __syncthreads();
+        if (e < experts) {
+            uint32_t n = 0u;
+            for (int w = 0; w < kSortWaves; ++w) n += in_wave[w][e];
+            next[e] += n;
+        }
+        __syncthreads();
+    }
+}
+
+__device__ __forceinline__ u32x4 narrow8(const float (&f)[8]) {
+    u32x4 v;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = bf16_of(f[2 * j]) | (bf16_of(f[2 * j + 1]) << 16);
+    return v;
+}
+
+constexpr int kRowSpan = 1024;          // elements of a row that one wave moves: two chunks per lane
+
+__global__ __launch_bounds__(256) void k_expert_gather(const uint16_t* x, int64_t ld_x, int64_t d, MxOrder o, uint16_t* xs, int64_t ld_xs) {
+    const int64_t slot = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (slot >= o.capacity) return;
+    const uint32_t choice = (uint32_t)o.src[slot], choices = (uint32_t)o.tokens * (uint32_t)o.top_k;
+    const uint16_t* row = choice < choices ? x + (int64_t)(choice / (uint32_t)o.top_k) * ld_x : nullptr;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int64_t c = (int64_t)blockIdx.y * kRowSpan + h * 512 + (threadIdx.x & 63) * 8;
+        if (c < d) store8(xs + slot * ld_xs, c, d, row ? load8(row, c, d) : u32x4{0u, 0u, 0u, 0u});
+    }
+}
+
+template <bool WEIGHTS>
+__global__ __launch_bounds__(256) void k_expert_combine(const uint16_t* ys, int64_t ld_ys, int64_t d, MxOrder o, const float* weights,
+                                                        uint16_t* y, int64_t ld_y) {
+    const int64_t token = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (token >= o.tokens) return;
+    float acc[2][8] = {};
+    for (int j = 0; j < o.top_k; ++j) {
+        const int64_t choice = token * o.top_k + j;
+        const uint32_t slot = (uint32_t)o.slot_of[choice];
+        if (slot >= (uint32_t)o.capacity) continue;
+        const float w = WEIGHTS ? weights[choice] : 1.0f;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int64_t c = (int64_t)blockIdx.y * kRowSpan + h * 512 + (threadIdx.x & 63) * 8;
+            if (c >= d) continue;
+            float f[8];
+            widen8(load8(ys + slot * ld_ys, c, d), f);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) acc[h][i] += WEIGHTS ? w * f[i] : f[i];
+        }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int64_t c = (int64_t)blockIdx.y * kRowSpan + h * 512 + (threadIdx.x & 63) * 8;
+        if (c < d) store8(y + token * ld_y, c, d, narrow8(acc[h]));
+    }
+}
+
+// One wave per slot.  The lanes' partial sums are joined in a fixed order.
+template <bool DYS, bool DW>
+__global__ __launch_bounds__(256) void k_expert_combine_backward(const uint16_t* dy, int64_t ld_dy, const uint16_t* ys, int64_t ld_ys, int64_t d,
+                                                                 MxOrder o, const float* weights, uint16_t* dys, int64_t ld_dys, float* dweights) {
+    const int64_t choices = (int64_t)o.tokens * o.top_k;
+    if (DW) {                           // dropped choices have no slot: their zeros are shared out over all lanes
+        const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+        if (i < choices && (uint32_t)o.slot_of[i] >= (uint32_t)o.capacity) dweights[i] = 0.0f;
+    }
+    const int64_t slot = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (slot >= o.capacity) return;
+    const uint32_t choice = (uint32_t)o.src[slot];
+    const bool used = choice < (uint64_t)choices;
+    if (!used && !DYS) return;
+    const uint16_t* row = used ? dy + (int64_t)(choice / (uint32_t)o.top_k) * ld_dy : nullptr;
+    const float w = DYS && used ? weights[choice] : 0.0f;
+    float sum = 0.0f;
+    for (int64_t c = (threadIdx.x & 63) * 8; c < d; c += 512) {
+        float g[8] = {};
+        if (used) widen8(load8(row, c, d), g);
+        if (DW && used) {
+            float f[8];
+            widen8(load8(ys + slot * ld_ys, c, d), f);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum = __builtin_fmaf(g[i], f[i], sum);
+        }
+        if (DYS) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) g[i] = used ? g[i] * w : 0.0f;
+            store8(dys + slot * ld_dys, c, d, narrow8(g));
+        }
+    }
+    if (DW && used) {
+#pragma unroll
+        for (int s = 32; s; s >>= 1) sum += __shfl_xor(sum, s);
+        if ((threadIdx.x & 63) == 0) dweights[choice] = sum;
+    }
+}
+
+uint32_t four_per_block(int64_t n) { return (uint32_t)((n + 3) / 4); }
+uint32_t row_spans(int64_t d) { return (uint32_t)((d + kRowSpan - 1) / kRowSpan); }
+
+}  // namespace
+
+size_t mx_sort_workspace(int64_t choices, int64_t n_experts) {
+    const int64_t chunks = (choices + kSortChunk - 1) / kSortChunk;
+    return chunks <= 1 ? 0 : (size_t)(chunks * n_experts * 4 + 15) / 16 * 16;
+}
+
+hipError_t launch_expert_sort(const int32_t* ids, const MxOrder& o, void* workspace, hipStream_t st) {
+    const int64_t choices = (int64_t)o.tokens * o.top_k;
+    const int64_t chunks = (choices + kSortChunk - 1) / kSortChunk;
+    if (chunks <= 1) {
+        k_expert_place<true><<<dim3(1), dim3(kSortThreads), 0, st>>>(ids, choices, nullptr, o);
+    } else {
+        uint32_t* counts = static_cast<uint32_t*>(workspace);
+        k_expert_count<<<dim3((uint32_t)chunks), dim3(kSortThreads), 0, st>>>(ids, choices, (uint32_t)o.n_experts, counts);
+        k_expert_place<false><<<dim3((uint32_t)chunks), dim3(kSortThreads), 0, st>>>(ids, choices, counts, o);
+    }
+    return hipGetLastError();
+}
+
+hipError_t launch_expert_gather(const uint16_t* x, int64_t ld_x, int64_t d, const MxOrder& o, uint16_t* xs, int64_t ld_xs, hipStream_t st) {
+    k_expert_gather<<<dim3(four_per_block(o.capacity), row_spans(d)), dim3(256), 0, st>>>(x, ld_x, d, o, xs, ld_xs);
+    return hipGetLastError();
+}
+
+hipError_t launch_expert_combine(const uint16_t* ys, int64_t ld_ys, int64_t d, const MxOrder& o, const float* weights, uint16_t* y,
+                                 int64_t ld_y, hipStream_t st) {
+    const dim3 grid(four_per_block(o.tokens), row_spans(d));
+    if (weights) k_expert_combine<true><<<grid, dim3(256), 0, st>>>(ys, ld_ys, d, o, weights, y, ld_y);
+    else k_expert_combine<false><<<grid, dim3(256), 0, st>>>(ys, ld_ys, d, o, weights, y, ld_y);
+    return hipGetLastError();
+}
+
+hipError_t launch_expert_combine_backward(const uint16_t* dy, int64_t ld_dy, const uint16_t* ys, int64_t ld_ys, int64_t d, const MxOrder& o,
+                                          const float* weights, uint16_t* dys, int64_t ld_dys, float* dweights, hipStream_t st) {
+    const dim3 grid(four_per_block(o.capacity));
+    if (dys && dweights) k_expert_combine_backward<true, true><<<grid, dim3(256), 0, st>>>(dy, ld_dy, ys, ld_ys, d, o, weights, dys, ld_dys, dweights);
+    else if (dys) k_expert_combine_backward<true, false><<<grid, dim3(256), 0, st>>>(dy, ld_dy, ys, ld_ys, d, o, weights, dys, ld_dys, dweights);
+    else k_expert_combine_backward<false, true><<<grid, dim3(256), 0, st>>>(dy, ld_dy, ys, ld_ys, d, o, weights, dys, ld_dys, dweights);
+    return hipGetLastError();
+}
+
+}  // namespace mor

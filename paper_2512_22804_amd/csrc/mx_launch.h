@@ -1,0 +1,68 @@
+// Host-side launch interface between the C ABI of the microscaled 4-bit operands (mx_api.hip) and their kernels.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace mor {
+
+constexpr int kMxBlock = 32;            // elements per scale
+
+// A packed operand on the device: codes and E8M0 bytes, leading dimensions and batch distances in bytes.
+struct MxOperand {
+    uint8_t* codes;  int64_t ld;
+    uint8_t* scales; int64_t ld_s;
+    int64_t  batch, batch_s;
+};
+
+// The order of tokens by expert, as the kernels see it.
+struct MxOrder {
+    int32_t  tokens, top_k, n_experts, align, capacity;
+    int32_t* offsets;
+    int32_t* slot_of;
+    int32_t* src;
+};
+
+struct MxQuantArgs {
+    const uint16_t* x;
+    int64_t  rows, cols, ld, batch_x;   // rows of the output (slots when `src` is set)
+    int32_t  batch;
+    const int32_t* src;                 // choice of each row, or nullptr: row r of x is row r
+    uint32_t choices, top_k;
+    const float* weights;               // factor of each choice, or nullptr
+    int      ceil_rule;
+    int      stochastic;
+    uint64_t seed;
+    MxOperand out, out_t;               // codes == nullptr: form not wanted
+};
+hipError_t launch_mx_quantize(const MxQuantArgs& a, hipStream_t st);
+hipError_t launch_mx_dequantize(int64_t rows, int64_t cols, int64_t batch, const MxOperand& op, uint16_t* y, int64_t ld_y, int64_t batch_y,
+                                hipStream_t st);
+
+// Products: which rows and which depth a workgroup's tile covers.
+enum { kMxDense = 0,      // one product
+       kMxRows = 1,       // rows of A and C: the segment of an expert; B: that expert's operand of the batch
+       kMxDepth = 2 };    // depth: the segment of an expert; C: that expert's result
+struct MxProductArgs {
+    const uint8_t* a;  int64_t lda;  const uint8_t* as; int64_t lda_s;
+    const uint8_t* b;  int64_t ldb;  const uint8_t* bs; int64_t ldb_s;
+    int64_t  batch_b, batch_bs;         // bytes between the experts' B (kMxRows)
+    void*    c;        int64_t ldc, batch_c;   // elements
+    int64_t  m, n;
+    int32_t  blocks;                    // blocks of 32 along the depth
+    const int32_t* offsets;             // experts' segments (kMxRows, kMxDepth)
+    int32_t  n_experts;
+    int32_t  f32;                       // C in binary32, else BF16
+};
+size_t mx_product_workspace(int64_t m, int64_t n, int64_t blocks);
+hipError_t launch_mx_product(int mode, const MxProductArgs& p, void* workspace, hipStream_t st);
+
+size_t mx_sort_workspace(int64_t choices, int64_t n_experts);
+hipError_t launch_expert_sort(const int32_t* ids, const MxOrder& o, void* workspace, hipStream_t st);
+hipError_t launch_expert_gather(const uint16_t* x, int64_t ld_x, int64_t d, const MxOrder& o, uint16_t* xs, int64_t ld_xs, hipStream_t st);
+hipError_t launch_expert_combine(const uint16_t* ys, int64_t ld_ys, int64_t d, const MxOrder& o, const float* weights, uint16_t* y,
+                                 int64_t ld_y, hipStream_t st);
+hipError_t launch_expert_combine_backward(const uint16_t* dy, int64_t ld_dy, const uint16_t* ys, int64_t ld_ys, int64_t d, const MxOrder& o,
+                                          const float* weights, uint16_t* dys, int64_t ld_dys, float* dweights, hipStream_t st);
+
+}  // namespace mor

@@ -1,0 +1,201 @@
+// Quantisation of BF16 operands to microscaled 4 bits (rows, transposed, or both from one read) and back.
+#include "mx_device.h"
+#include "mx_launch.h"
+
+namespace mor {
+namespace {
+
+constexpr int kTileCols = 128;          // columns of a workgroup's tile: 16 lanes of 8 elements
+
+// One workgroup: RPT * 16 rows x 128 columns, 256 lanes.  Lane t holds 8 columns (16 bytes) of RPT rows; a block of the row
+// form is then 4 neighbouring lanes.  For the transposed form the tile goes through LDS (T: RPT = 8), and lane t takes a pair
+// of columns over 32 rows, so that a block's amax needs no other lane and its 16 bytes are one store; four neighbouring
+// lanes fill 64 bytes of an output row.  The rows of row block q are rotated by 16 q dwords: the four row blocks that
+// neighbouring lanes read then lie in different banks.
+template <int RPT, bool ROWS, bool T, bool SR, bool WEIGHTED>
+__global__ __launch_bounds__(256) void k_mx_quantize(MxQuantArgs a, uint32_t col_tiles) {
+    static_assert(!T || RPT == 8, "the transposed form works on 128 x 128 tiles");
+    __shared__ __align__(16) uint32_t tile[T ? 128 * 64 : 4];
+    __shared__ float row_weight[WEIGHTED ? RPT * 16 : 1];
+    const int t = threadIdx.x;
+    const uint32_t ct = blockIdx.x % col_tiles;
+    const int64_t rt = blockIdx.x / col_tiles;
+    const int64_t c0 = (int64_t)ct * kTileCols, r0 = rt * (RPT * 16);
+    const uint32_t z = blockIdx.z;
+    const uint16_t* x = a.x + (int64_t)z * a.batch_x;
+    const int64_t c = c0 + (t & 15) * 8;
+    const uint32_t k0 = (uint32_t)a.seed, k1 = (uint32_t)(a.seed >> 32);
+
+    u32x4 v[RPT];
+    float w[RPT];
+#pragma unroll
+    for (int i = 0; i < RPT; ++i) {
+        const int64_t r = r0 + (t >> 4) + 16 * i;
+        const uint16_t* row = nullptr;
+        w[i] = 1.0f;
+        if (r < a.rows) {
+            if (a.src == nullptr) row = x + r * a.ld;
+            else {
+                const uint32_t choice = (uint32_t)a.src[r];
+                if (choice < a.choices) {
+                    row = x + (int64_t)(choice / a.top_k) * a.ld;
+                    if (WEIGHTED) w[i] = a.weights[choice];
+                }
+            }
+        }
+        v[i] = row != nullptr && c < a.cols ? load8(row, c, a.cols) : u32x4{0u, 0u, 0u, 0u};
+    }
+    const bool ceil_rule = a.ceil_rule != 0;
+    if (T) {
+#pragma unroll
+        for (int i = 0; i < RPT; ++i) {
+            const int r = (t >> 4) + 16 * i;
+            *reinterpret_cast<u32x4*>(&tile[r * 64 + (((t & 15) * 4 + 16 * (r >> 5)) & 63)]) = v[i];
+            if (WEIGHTED && (t & 15) == 0) row_weight[r] = w[i];
+        }
+    }
+    if (ROWS) {
+        const MxOperand o = a.out;
+        const int64_t block = c / kMxBlock;
+        const bool inside = block * kMxBlock < a.cols;
+#pragma unroll
+        for (int i = 0; i < RPT; ++i) {
+            const int64_t r = r0 + (t >> 4) + 16 * i;
+            uint32_t amax;
+            float f[8];
+            if (SR || WEIGHTED) widen8(v[i], f);
+            if (WEIGHTED) {
+                amax = 0u;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    f[j] = c + j < a.cols ? f[j] * w[i] : 0.0f;         // what a row lacks stays +0 under a negative weight
+                    amax = max(amax, __float_as_uint(f[j]) & 0x7FFFFFFFu);
+                }
+            } else {
+                uint32_t m = 0u;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) m = pk_max_u16(m, v[i][j] & 0x7FFF7FFFu);
+                amax = fold_max16(m) << 16;
+            }
+            amax = max(amax, (uint32_t)__shfl_xor((int)amax, 1));
+            amax = max(amax, (uint32_t)__shfl_xor((int)amax, 2));
+            const uint32_t byte = mx_scale_byte(amax, ceil_rule);
+            uint32_t codes;
+            if (SR) codes = mx_codes8_stochastic(f, byte, philox((uint32_t)(c >> 3), (uint32_t)r, z, 0u, k0, k1));
+            else if (WEIGHTED) codes = mx_codes8_nearest(f, byte);
+            else codes = mx_codes8_nearest(v[i], byte);
+            if (r < a.rows && inside) {
+                *reinterpret_cast<uint32_t*>(o.codes + z * o.batch + r * o.ld + (c >> 1)) = codes;
+                if ((t & 3) == 0) o.scales[z * o.batch_s + r * o.ld_s + block] = (uint8_t)byte;
+            }
+        }
+    }
+    if (T) {
+        const MxOperand o = a.out_t;
+        __syncthreads();
+        const int q = t & 3, pair = t >> 2;
+        const int64_t col = c0 + 2 * pair, row0 = r0 + 32 * q;
+        uint32_t d[32];
+        uint32_t m = 0u;
+        float wa = 0.0f;
+        uint32_t amax0 = 0u, amax1 = 0u;
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+            d[j] = tile[(32 * q + j) * 64 + ((pair + 16 * q) & 63)];
+            if (WEIGHTED) {
+                wa = row_weight[32 * q + j];
+                amax0 = max(amax0, __float_as_uint(__uint_as_float(d[j] << 16) * wa) & 0x7FFFFFFFu);
+                amax1 = max(amax1, __float_as_uint(__uint_as_float(d[j] & 0xFFFF0000u) * wa) & 0x7FFFFFFFu);
+            } else m = pk_max_u16(m, d[j] & 0x7FFF7FFFu);
+        }
+        if (!WEIGHTED) { amax0 = m << 16; amax1 = m & 0xFFFF0000u; }
+#pragma unroll
+        for (int side = 0; side < 2; ++side) {
+            const uint32_t byte = mx_scale_byte(side ? amax1 : amax0, ceil_rule);
+            u32x4 codes;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                if (SR || WEIGHTED) {
+                    float f[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        f[j] = __uint_as_float(side ? (d[8 * g + j] & 0xFFFF0000u) : (d[8 * g + j] << 16));
+                        if (WEIGHTED) f[j] *= row_weight[32 * q + 8 * g + j];
+                    }
+                    if (SR) codes[g] = mx_codes8_stochastic(f, byte, philox((uint32_t)(row0 >> 3) + g, (uint32_t)(col + side), z, 1u, k0, k1));
+                    else codes[g] = mx_codes8_nearest(f, byte);
+                } else {
+                    u32x4 p;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        p[j] = __builtin_amdgcn_perm(d[8 * g + 2 * j + 1], d[8 * g + 2 * j], side ? 0x07060302u : 0x05040100u);
+                    codes[g] = mx_codes8_nearest(p, byte);
+                }
+            }
+            if (col + side < a.cols && row0 < a.rows) {
+                *reinterpret_cast<u32x4*>(o.codes + z * o.batch + (col + side) * o.ld + (row0 >> 1)) = codes;
+                o.scales[z * o.batch_s + (col + side) * o.ld_s + (row0 >> 5)] = (uint8_t)byte;
+            }
+        }
+    }
+}
+
+// Eight codes to eight BF16 values per lane; the product with the scale is exact in binary32 and fits BF16 exactly.
+__global__ __launch_bounds__(256) void k_mx_dequantize(int64_t rows, int64_t cols, MxOperand op, uint16_t* y, int64_t ld_y, int64_t batch_y,
+                                                       uint32_t col_tiles) {
+    const uint32_t ct = blockIdx.x % col_tiles;
+    const int64_t c = (int64_t)ct * kTileCols + (threadIdx.x & 15) * 8;
+    const int64_t r = (int64_t)(blockIdx.x / col_tiles) * 16 + (threadIdx.x >> 4);
+    const uint32_t z = blockIdx.z;
+    if (r >= rows || c >= cols) return;
+    const uint32_t codes = *reinterpret_cast<const uint32_t*>(op.codes + z * op.batch + r * op.ld + (c >> 1));
+    const uint32_t byte = op.scales[z * op.batch_s + r * op.ld_s + (c >> 5)];
+    const float s = mx_scale_value(byte) * 0.5f;            // byte 0: 2^-128, a subnormal
+    u32x4 out;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const uint32_t code = codes >> (4 * j);
+        const float twice = (float)((uint32_t)(0x0C08060403020100ull >> (8 * (code & 7u))) & 0xFFu);
+        uint32_t b = (__float_as_uint(twice * s) >> 16) | ((code & 8u) << 12);
+        if (byte == kMxNan) b = 0x7FC0u;
+        out[j >> 1] = (j & 1) ? (out[j >> 1] | (b << 16)) : b;
+    }
+    store8(y + (int64_t)z * batch_y + r * ld_y, c, cols, out);
+}
+
+template <int RPT, bool ROWS, bool T>
+void quantize_form(const MxQuantArgs& a, uint32_t col_tiles, dim3 grid, hipStream_t st) {
+    if (a.stochastic) {
+        if (a.weights) k_mx_quantize<RPT, ROWS, T, true, true><<<grid, dim3(256), 0, st>>>(a, col_tiles);
+        else k_mx_quantize<RPT, ROWS, T, true, false><<<grid, dim3(256), 0, st>>>(a, col_tiles);
+    } else {
+        if (a.weights) k_mx_quantize<RPT, ROWS, T, false, true><<<grid, dim3(256), 0, st>>>(a, col_tiles);
+        else k_mx_quantize<RPT, ROWS, T, false, false><<<grid, dim3(256), 0, st>>>(a, col_tiles);
+    }
+}
+
+}  // namespace
+
+hipError_t launch_mx_quantize(const MxQuantArgs& a, hipStream_t st) {
+    const uint32_t col_tiles = (uint32_t)((a.cols + kTileCols - 1) / kTileCols);
+    const bool rows_form = a.out.codes != nullptr, t_form = a.out_t.codes != nullptr;
+    const int tile_rows = t_form ? 128 : 16;
+    const int64_t tiles = ((a.rows + tile_rows - 1) / tile_rows) * col_tiles;
+    if (tiles > 0x7FFFFFFFll) return hipErrorInvalidValue;
+    const dim3 grid((uint32_t)tiles, 1, (uint32_t)a.batch);
+    if (!t_form) quantize_form<1, true, false>(a, col_tiles, grid, st);
+    else if (rows_form) quantize_form<8, true, true>(a, col_tiles, grid, st);
+    else quantize_form<8, false, true>(a, col_tiles, grid, st);
+    return hipGetLastError();
+}
+
+hipError_t launch_mx_dequantize(int64_t rows, int64_t cols, int64_t batch, const MxOperand& op, uint16_t* y, int64_t ld_y, int64_t batch_y,
+                                hipStream_t st) {
+    const uint32_t col_tiles = (uint32_t)((cols + kTileCols - 1) / kTileCols);
+    const int64_t tiles = ((rows + 15) / 16) * col_tiles;
+    if (tiles > 0x7FFFFFFFll) return hipErrorInvalidValue;
+    k_mx_dequantize<<<dim3((uint32_t)tiles, 1, (uint32_t)batch), dim3(256), 0, st>>>(rows, cols, op, y, ld_y, batch_y, col_tiles);
+    return hipGetLastError();
+}
+
+}  // namespace mor
