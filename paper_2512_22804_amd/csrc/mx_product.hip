@@ -84,6 +84,12 @@ __device__ __forceinline__ bool find_tile(const MxProductArgs& p, uint32_t m_til
     return true;
 }
 
+__device__ __forceinline__ u32x2 narrow4(const f32x4& v) {
+    typedef float f32x2_t __attribute__((ext_vector_type(2)));
+    const bf16x2 low = __builtin_convertvector((f32x2_t{v[0], v[1]}), bf16x2), high = __builtin_convertvector((f32x2_t{v[2], v[3]}), bf16x2);
+    return u32x2{__builtin_bit_cast(uint32_t, low), __builtin_bit_cast(uint32_t, high)};
+}
+
 // Four consecutive elements of a row of C.
 __device__ __forceinline__ void store4(const MxProductArgs& p, int64_t at, int64_t n, const f32x4& v) {
     if (p.f32) {
@@ -95,7 +101,7 @@ __device__ __forceinline__ void store4(const MxProductArgs& p, int64_t at, int64
     } else {
         uint16_t* c = reinterpret_cast<uint16_t*>(p.c) + at;
         if (n + 4 <= p.n) {
-            const u32x2 w{bf16_of(v[0]) | (bf16_of(v[1]) << 16), bf16_of(v[2]) | (bf16_of(v[3]) << 16)};
+            const u32x2 w = narrow4(v);
             __builtin_memcpy(c, &w, 8);
         }
         else
@@ -166,8 +172,6 @@ __global__ __launch_bounds__(64) void k_mx_product(MxProductArgs p, uint32_t n_t
 // in the last stage, and stages beyond the last, whose range is empty.  The scale bytes behind the last block, loaded four at
 // a time, are replaced by 2^0: whatever they hold, a NaN too, counts for nothing.
 
-typedef __attribute__((address_space(3))) void lds_void;
-
 constexpr uint32_t kNowhere = 0x7FFFFFFFu;              // an offset that no range contains
 
 // Bytes `first` .. `row_bytes` - 1 of an operand's rows row0 .. row0 + rows - 1, advancing along the rows.  The same in every lane:
@@ -182,16 +186,29 @@ struct RowsBuffer {
         base = reinterpret_cast<const uint8_t*>(((uint64_t)high << 32) | low);
         bytes = __builtin_amdgcn_readfirstlane(rows > 0 && row_bytes > first ? (int)((rows - 1) * ld + row_bytes - first) : 0);
     }
-    __device__ __forceinline__ __amdgpu_buffer_rsrc_t at(int step, bool exists) const {
-        return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base) + step, 0, exists ? max(bytes - step, 0) : 0, 0x00020000);
+    // The buffer resource from byte `step` of every row on.
+    __device__ __forceinline__ u32x4 at(int step, bool exists) const {
+        const uint64_t p = reinterpret_cast<uint64_t>(base) + step;
+        return u32x4{(uint32_t)p, (uint32_t)(p >> 32) & 0xFFFFu, exists ? (uint32_t)max(bytes - step, 0) : 0u, 0x00020000u};
     }
 };
+
+// 16 bytes per lane from a buffer straight into LDS, one lane behind the other from `lds` on.  Written out because the compiler
+// tracks the builtin's writes into LDS and, not being able to tell the four buffers apart across the loop, waits for all requests
+// before it reads any buffer.  Nothing is loaded into registers here, and the waits stand in multiply_stage.  (M0 is a reserved
+// register: the compiler sets it right before each use of its own, and nothing else in this kernel uses it.)
+__device__ __forceinline__ void load_to_lds(uint8_t* lds, u32x4 buffer, uint32_t offset, int group_offset) {
+    const uint32_t to = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) uint8_t*)lds);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+                 : : "s"(to), "v"(offset), "s"(buffer), "s"(group_offset) : "memory");
+}
 
 template <int BM, int BN>
 struct TileShape {
     static constexpr int FM = BM / 32, FN = BN / 32;    // fragments of 16 rows of a wave
-    static constexpr int kCodesB = BM * 64, kScalesA = (BM + BN) * 64, kScalesB = kScalesA + BM * 4, kBytes = kScalesB + BN * 4;
-    static constexpr int kRequests = (BM + BN) / 64 + (BM + BN) / 256;      // of one wave and stage
+    static constexpr int kCodesB = BM * 64, kCodes = (BM + BN) * 64;            // bytes of a stage
+    static constexpr int kScalesB = BM * 16, kScales = (BM + BN) * 16;          // bytes of four stages
+    static constexpr int kRequests = kCodes / 4096, kScaleRequests = kScales / 4096;     // of one wave
 };
 
 // What a lane adds to the stage's base to request its pieces.
@@ -199,108 +216,177 @@ struct Request {
     RowsBuffer a, as, b, bs;
     uint32_t va, vb, vas, vbs;          // offset in the first group of rows
     uint32_t va_last, vb_last;          // the same in the last stage
-    int step_a, step_b, step_as, step_bs;       // bytes between the groups of a wave
+    int step_a, step_b;                 // bytes between the groups of a wave
     int last;
 };
 
-// Wave w loads the codes of rows 16 (w + 4 i) .. + 15 and the scales of rows 64 (w + 4 i) .. + 63.
+// Wave w loads the codes of rows 16 (w + 4 i) .. + 15 of one stage.
 template <int BM, int BN>
-__device__ __forceinline__ void request_stage(uint8_t* lds, const Request& q, int stage, int wave) {
+__device__ __forceinline__ void request_codes(uint8_t* lds, const Request& q, int stage, int wave) {
     typedef TileShape<BM, BN> S;
     const bool exists = stage <= q.last;
-    const __amdgpu_buffer_rsrc_t ra = q.a.at(stage * 64, exists), rb = q.b.at(stage * 64, exists);
-    const __amdgpu_buffer_rsrc_t ras = q.as.at(stage * 4, exists), rbs = q.bs.at(stage * 4, exists);
+    const u32x4 ra = q.a.at(stage * 64, exists), rb = q.b.at(stage * 64, exists);
     const uint32_t va = stage == q.last ? q.va_last : q.va, vb = stage == q.last ? q.vb_last : q.vb;
 #pragma unroll
     for (int i = 0; i < BM / 64; ++i)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_void*)(lds + (wave + 4 * i) * 1024), 16, va, i * q.step_a, 0, 0);
+        load_to_lds(lds + (wave + 4 * i) * 1024, ra, va, i * q.step_a);
 #pragma unroll
     for (int i = 0; i < BN / 64; ++i)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_void*)(lds + S::kCodesB + (wave + 4 * i) * 1024), 16, vb, i * q.step_b, 0, 0);
-    if (BM >= 256) __builtin_amdgcn_raw_ptr_buffer_load_lds(ras, (lds_void*)(lds + S::kScalesA + wave * 256), 4, q.vas, 0, 0, 0);
-    if (BN >= 256) __builtin_amdgcn_raw_ptr_buffer_load_lds(rbs, (lds_void*)(lds + S::kScalesB + wave * 256), 4, q.vbs, 0, 0, 0);
-    if (BM == 128 && BN == 128) {       // two waves the scales of A, two those of B, which follow them in LDS
-        if (wave < 2) __builtin_amdgcn_raw_ptr_buffer_load_lds(ras, (lds_void*)(lds + S::kScalesA + wave * 256), 4, q.vas, 0, 0, 0);
-        else __builtin_amdgcn_raw_ptr_buffer_load_lds(rbs, (lds_void*)(lds + S::kScalesA + wave * 256), 4, q.vbs, 0, 0, 0);
-    }
+        load_to_lds(lds + S::kCodesB + (wave + 4 * i) * 1024, rb, vb, i * q.step_b);
+}
+// The scales of four stages, 16 bytes of a row: every row is a request of its own to the caches, so four stages share it.  Wave w
+// loads those of rows 64 w .. + 63 of either operand, or of one of them where each has 128 rows.
+template <int BM, int BN>
+__device__ __forceinline__ void request_scales(uint8_t* lds, const Request& q, int stage, int wave) {
+    typedef TileShape<BM, BN> S;
+    static_assert(BM == BN && (BM == 256 || BM == 128), "which wave loads which rows");
+    const bool exists = stage <= q.last;
+    const u32x4 ra = q.as.at(stage * 4, exists), rb = q.bs.at(stage * 4, exists);
+    if (BM == 256 || wave < 2) load_to_lds(lds + wave * 1024, ra, q.vas, 0);
+    if (BM == 256) load_to_lds(lds + S::kScalesB + wave * 1024, rb, q.vbs, 0);
+    else if (wave >= 2) load_to_lds(lds + wave * 1024, rb, q.vbs, 0);
 }
 
 // A lane's places in a buffer.
 struct Place {
-    uint32_t a, b, sa, sb;
+    uint32_t a, b, sa, sb;              // in the codes' and the scales' buffers
 };
 
-template <int FM, int FN>
+template <int FN>
 struct Fragments {
     u32x4 a0, a1, b[FN];                // the first two of A
-    uint32_t sa[FM], sb[FN];
+};
+template <int FM, int FN>
+struct Scales {
+    uint32_t a[FM], b[FN];              // byte t: stage t of four
 };
 template <int BM, int BN>
-__device__ __forceinline__ void read_first(Fragments<BM / 32, BN / 32>& f, const uint8_t* lds, const Place& at) {
+__device__ __forceinline__ void read_first(Fragments<BN / 32>& f, const uint8_t* lds, const Place& at) {
 #pragma unroll
-    for (int j = 0; j < BN / 32; ++j) { f.b[j] = *reinterpret_cast<const u32x4*>(lds + at.b + j * 1024); f.sb[j] = lds[at.sb + j * 64]; }
+    for (int j = 0; j < BN / 32; ++j) f.b[j] = *reinterpret_cast<const u32x4*>(lds + at.b + j * 1024);
     f.a0 = *reinterpret_cast<const u32x4*>(lds + at.a);
     f.a1 = *reinterpret_cast<const u32x4*>(lds + at.a + 1024);
-#pragma unroll
-    for (int i = 0; i < BM / 32; ++i) f.sa[i] = lds[at.sa + i * 64];
+}
+// This lane's block of each stage: byte `part` of each of the four words; `keep` and `put` replace what lies behind the last block.
+__device__ __forceinline__ uint32_t scales_of(const uint8_t* lds, uint32_t select, uint32_t keep, uint32_t put) {
+    const u32x4 d = *reinterpret_cast<const u32x4*>(lds);
+    const uint32_t low = __builtin_amdgcn_perm(d[1], d[0], select), high = __builtin_amdgcn_perm(d[3], d[2], select);
+    return (__builtin_amdgcn_perm(high, low, 0x05040100u) & keep) | put;
 }
 
 // Four matrix instructions.  The compiler keeps the accumulators of a 128 x 128 wave in place only if told to: with the builtin it
 // gives sums and addends different registers, which do not suffice (256 of 512 are accumulators), and moves them about.  As it
 // does not look into the text, the two wait states between a vector instruction that writes an operand and a matrix instruction
 // that reads it stand there, and settle() below stands before the first other use of the sums.
-#define MOR_MFMA(C, B, SB) "v_mfma_scale_f32_16x16x128_f8f6f4 " C ", " B ", %8, " C ", " SB ", %13 op_sel_hi:[0,0,0] cbsz:4 blgp:4\n\t"
+// T: which byte of the scales.
+#define MOR_MFMA(C, B, SB, SEL) "v_mfma_scale_f32_16x16x128_f8f6f4 " C ", " B ", %8, " C ", " SB ", %13 " SEL " cbsz:4 blgp:4\n\t"
+#define MOR_MFMA4(SEL)                                                                                                                    \
+    asm("s_nop 1\n\t" MOR_MFMA("%0", "%4", "%9", SEL) MOR_MFMA("%1", "%5", "%10", SEL) MOR_MFMA("%2", "%6", "%11", SEL)                    \
+            MOR_MFMA("%3", "%7", "%12", SEL)                                                                                              \
+        : "+a"(c0), "+a"(c1), "+a"(c2), "+a"(c3)                                                                                          \
+        : "v"(b0), "v"(b1), "v"(b2), "v"(b3), "v"(a), "v"(sb0), "v"(sb1), "v"(sb2), "v"(sb3), "v"(sa))
+template <int T>
 __device__ __forceinline__ void mfma4(f32x4& c0, f32x4& c1, f32x4& c2, f32x4& c3, u32x4 a, uint32_t sa, u32x4 b0, u32x4 b1, u32x4 b2, u32x4 b3,
                                       uint32_t sb0, uint32_t sb1, uint32_t sb2, uint32_t sb3) {
-    asm("s_nop 1\n\t" MOR_MFMA("%0", "%4", "%9") MOR_MFMA("%1", "%5", "%10") MOR_MFMA("%2", "%6", "%11") MOR_MFMA("%3", "%7", "%12")
-        : "+a"(c0), "+a"(c1), "+a"(c2), "+a"(c3)
-        : "v"(b0), "v"(b1), "v"(b2), "v"(b3), "v"(a), "v"(sb0), "v"(sb1), "v"(sb2), "v"(sb3), "v"(sa));
+    if (T == 0) MOR_MFMA4("op_sel:[0,0,0] op_sel_hi:[0,0,0]");
+    else if (T == 1) MOR_MFMA4("op_sel:[1,1,0] op_sel_hi:[0,0,0]");
+    else if (T == 2) MOR_MFMA4("op_sel:[0,0,0] op_sel_hi:[1,1,0]");
+    else MOR_MFMA4("op_sel:[1,1,0] op_sel_hi:[1,1,0]");
 }
+#undef MOR_MFMA4
 #undef MOR_MFMA
 // The last matrix instructions (four passes of four cycles) have written their sums.
 __device__ __forceinline__ void settle(f32x4& c0, f32x4& c1, f32x4& c2, f32x4& c3) {
     asm volatile("s_nop 15\n\ts_nop 15" : "+a"(c0), "+a"(c1), "+a"(c2), "+a"(c3));
 }
 
-// One stage: `cur` holds its first fragments; `next` receives those of the stage in `lds_next`.
-template <int BM, int BN>
-__device__ __forceinline__ void multiply_stage(f32x4 (&acc)[BM / 32][BN / 32], Fragments<BM / 32, BN / 32>& cur, Fragments<BM / 32, BN / 32>& next,
-                                               const uint8_t* lds, const uint8_t* lds_next, uint8_t* lds_free, const Place& at, const Request& q,
-                                               int stage, int wave, bool keep_last) {
-    constexpr int FM = BM / 32, FN = BN / 32, kRequests = TileShape<BM, BN>::kRequests;
+// Stage T of four: `cur` holds its first fragments; `next` receives those of the stage in `lds_next`.  Stage 0 requests the scales
+// of the four stages after its own, stage 3 reads them.
+template <int T, int BM, int BN>
+__device__ __forceinline__ void multiply_stage(f32x4 (&acc)[BM / 32][BN / 32], Fragments<BN / 32>& cur, Fragments<BN / 32>& next,
+                                               Scales<BM / 32, BN / 32>& scales, const uint8_t* lds, const uint8_t* lds_next, uint8_t* lds_free,
+                                               uint8_t* lds_scales, const Place& at, const Request& q, int stage, int wave, uint32_t select,
+                                               uint32_t keep_last, uint32_t put_last) {
+    typedef TileShape<BM, BN> S;
+    constexpr int FM = S::FM, FN = S::FN;
     static_assert(FM == FN, "one fragment of each operand is read per step");
-    __builtin_amdgcn_s_waitcnt(0x0F70 | kRequests);     // all but the latest stage's requests have arrived
+    __builtin_amdgcn_s_waitcnt(0x0F70 | (S::kRequests + (T == 1 ? S::kScaleRequests : 0)));     // all but the latest stage's requests are here
     __syncthreads();
-    request_stage<BM, BN>(lds_free, q, stage + 3, wave);
-    const bool keep = stage + 1 < q.last || keep_last;
+    request_codes<BM, BN>(lds_free, q, stage + 3, wave);
+    if (T == 0) request_scales<BM, BN>(lds_scales, q, stage + 4, wave);
+    const bool last_four = stage + 4 >= q.last;         // (T == 3) stages s + 1 .. s + 4 hold the last one
+    const uint32_t keep = last_four ? keep_last : 0xFFFFFFFFu, put = last_four ? put_last : 0u;
     u32x4 a0 = cur.a0, a1 = cur.a1;
+    Scales<FM, FN> fresh;
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
         const u32x4 a = a0;
         a0 = a1;
         a1 = *reinterpret_cast<const u32x4*>(i + 2 < FM ? lds + at.a + (i + 2) * 1024 : lds_next + at.a + (i + 2 - FM) * 1024);
         next.b[i] = *reinterpret_cast<const u32x4*>(lds_next + at.b + i * 1024);
-        const uint32_t sb = lds_next[at.sb + i * 64], sa = lds_next[at.sa + i * 64];
-        next.sb[i] = keep ? sb : 127u;
-        next.sa[i] = keep ? sa : 127u;
+        if (T == 3) {
+            fresh.a[i] = scales_of(lds_scales + at.sa + i * 256, select, keep, put);
+            fresh.b[i] = scales_of(lds_scales + at.sb + i * 256, select, keep, put);
+        }
 #pragma unroll
         for (int j = 0; j < FN; j += 4)
-            mfma4(acc[i][j], acc[i][j + 1], acc[i][j + 2], acc[i][j + 3], a, cur.sa[i], cur.b[j], cur.b[j + 1], cur.b[j + 2], cur.b[j + 3],
-                  cur.sb[j], cur.sb[j + 1], cur.sb[j + 2], cur.sb[j + 3]);
+            mfma4<T>(acc[i][j], acc[i][j + 1], acc[i][j + 2], acc[i][j + 3], a, scales.a[i], cur.b[j], cur.b[j + 1], cur.b[j + 2], cur.b[j + 3],
+                     scales.b[j], scales.b[j + 1], scales.b[j + 2], scales.b[j + 3]);
         __builtin_amdgcn_sched_barrier(0);      // the reads stay spread over the matrix instructions
     }
     next.a0 = a0;
     next.a1 = a1;
+    if (T == 3) scales = fresh;
 }
 
-template <int MODE, int BM, int BN>
+// A wave's sums to C by way of its LDS buffer, so that every row is written in pieces of 16 neighbouring bytes per lane: the
+// accumulators hold 4 columns of 16 rows.  `kCols` columns at a time; pieces lie permuted by the row against bank conflicts.
+template <bool F32, int FM, int FN>
+__device__ __forceinline__ void store_tile(const MxProductArgs& p, uint8_t* lds, f32x4 (&acc)[FM][FN], int64_t base, int64_t m0, int64_t m_end,
+                                           int64_t n0, int lane) {
+    constexpr int kSize = F32 ? 4 : 2;
+    constexpr int kCols = FN * 16 * kSize > 256 ? 256 / kSize : FN * 16;        // a row of up to 256 bytes
+    constexpr int kRow = kCols * kSize, kPieces = kRow / 16, kLanes = 64 / kPieces;
+    const int row = lane & 15, part = lane >> 4;
+#pragma unroll
+    for (int c0 = 0; c0 < FN * 16; c0 += kCols) {
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < kCols / 16; ++j) {
+                const f32x4 v = acc[i][c0 / 16 + j];
+                uint8_t* at = lds + (16 * i + row) * kRow;
+                if (F32) *reinterpret_cast<f32x4*>(at + ((4 * j + part) ^ (row & (kPieces - 1))) * 16) = v;
+                else *reinterpret_cast<u32x2*>(at + ((2 * j + (part >> 1)) ^ (row & (kPieces - 1))) * 16 + (part & 1) * 8) = narrow4(v);
+            }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        const int piece = lane % kPieces;
+        const int64_t n = n0 + c0 + piece * (16 / kSize);
+#pragma unroll 4
+        for (int r = lane / kPieces; r < FM * 16; r += kLanes) {
+            const u32x4 v = *reinterpret_cast<const u32x4*>(lds + r * kRow + (piece ^ (r & (kPieces - 1))) * 16);
+            if (m0 + r >= m_end || n >= p.n) break;
+            uint8_t* c = reinterpret_cast<uint8_t*>(p.c) + (base + (m0 + r) * p.ldc + n) * kSize;
+            if (n + 16 / kSize <= p.n) __builtin_memcpy(c, &v, 16);
+            else {
+#pragma unroll 1
+                for (int e = 0; n + e < p.n; ++e)       // the last columns
+                    __builtin_memcpy(c + e * kSize, lds + r * kRow + (piece ^ (r & (kPieces - 1))) * 16 + e * kSize, kSize);
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+}
+
+template <int MODE, bool F32, int BM, int BN>
 __global__ __launch_bounds__(256, 1) void k_mx_tile(MxProductArgs p, uint32_t m_tiles, uint32_t n_tiles) {
     typedef TileShape<BM, BN> S;
     constexpr int FM = S::FM, FN = S::FN;
-    __shared__ __align__(1024) uint8_t buf0[S::kBytes];
-    __shared__ __align__(1024) uint8_t buf1[S::kBytes];
-    __shared__ __align__(1024) uint8_t buf2[S::kBytes];
-    __shared__ __align__(1024) uint8_t buf3[S::kBytes];
+    __shared__ __align__(1024) uint8_t buf0[S::kCodes];
+    __shared__ __align__(1024) uint8_t buf1[S::kCodes];
+    __shared__ __align__(1024) uint8_t buf2[S::kCodes];
+    __shared__ __align__(1024) uint8_t buf3[S::kCodes];
+    __shared__ __align__(1024) uint8_t buf_scales[S::kScales];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // Workgroups go to the eight XCDs in turn; each XCD takes a run of tiles, in patches of 8 tile rows, so that the tiles at work
     // together share their operands in its L2.
@@ -330,63 +416,64 @@ __global__ __launch_bounds__(256, 1) void k_mx_tile(MxProductArgs p, uint32_t m_
               RowsBuffer(p.bs + of_bs, p.ldb_s, n0, rows_b, t.k0, row_scales),
               (uint32_t)(wave * 16 + (lane >> 2)) * (uint32_t)p.lda + piece * 16, (uint32_t)(wave * 16 + (lane >> 2)) * (uint32_t)p.ldb + piece * 16,
               (uint32_t)(wave * 64 + lane) * (uint32_t)p.lda_s, (uint32_t)((BM == 128 ? wave - 2 : wave) * 64 + lane) * (uint32_t)p.ldb_s, 0u, 0u,
-              (int)p.lda * 64, (int)p.ldb * 64, (int)p.lda_s * 256, (int)p.ldb_s * 256, stages - 1};
+              (int)p.lda * 64, (int)p.ldb * 64, stages - 1};
     q.va_last = piece_in ? q.va : kNowhere;
     q.vb_last = piece_in ? q.vb : kNowhere;
 
     const int row = lane & 15, part = lane >> 4;
     const int wm = (wave >> 1) * (BM / 2), wn = (wave & 1) * (BN / 2);
     const uint32_t at_piece = (part ^ (row >> 1 & 3)) * 16;
-    const Place at{(uint32_t)(wm + row) * 64 + at_piece, (uint32_t)S::kCodesB + (wn + row) * 64 + at_piece,
-                   (uint32_t)S::kScalesA + (wm + row) * 4 + part, (uint32_t)S::kScalesB + (wn + row) * 4 + part};
-    const bool keep_last = (stages - 1) * 4 + part < blocks;
+    const Place at{(uint32_t)(wm + row) * 64 + at_piece, (uint32_t)S::kCodesB + (wn + row) * 64 + at_piece, (uint32_t)(wm + row) * 16,
+                   (uint32_t)S::kScalesB + (wn + row) * 16};
+    const uint32_t select = (uint32_t)part | ((uint32_t)(part + 4) << 8);
+    // the last four stages' scales: bytes of this lane's blocks that exist
+    uint32_t keep_last = 0u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (((stages - 1) / 4 * 4 + i) * 4 + part < blocks) keep_last |= 0xFFu << (8 * i);
+    const uint32_t put_last = 0x7F7F7F7Fu & ~keep_last;
 
     f32x4 acc[FM][FN] = {};
     if (stages > 0) {
-        Fragments<FM, FN> f0, f1;
-        request_stage<BM, BN>(buf0, q, 0, wave);
-        request_stage<BM, BN>(buf1, q, 1, wave);
-        request_stage<BM, BN>(buf2, q, 2, wave);
+        Fragments<FN> f0, f1;
+        Scales<FM, FN> sc;
+        request_scales<BM, BN>(buf_scales, q, 0, wave);
+        request_codes<BM, BN>(buf0, q, 0, wave);
+        request_codes<BM, BN>(buf1, q, 1, wave);
+        request_codes<BM, BN>(buf2, q, 2, wave);
         __builtin_amdgcn_s_waitcnt(0x0F70 | (2 * S::kRequests & 15) | (2 * S::kRequests >> 4 << 14));
         __syncthreads();
         read_first<BM, BN>(f0, buf0, at);
-        if (stages == 1 && !keep_last) {
+        const uint32_t keep = stages <= 4 ? keep_last : 0xFFFFFFFFu, put = stages <= 4 ? put_last : 0u;
 #pragma unroll
-            for (int i = 0; i < FM; ++i) f0.sa[i] = 127u;
-#pragma unroll
-            for (int j = 0; j < FN; ++j) f0.sb[j] = 127u;
+        for (int i = 0; i < FM; ++i) {
+            sc.a[i] = scales_of(buf_scales + at.sa + i * 256, select, keep, put);
+            sc.b[i] = scales_of(buf_scales + at.sb + i * 256, select, keep, put);
         }
         // (One way out of the loop: with more the compiler moves accumulators between registers.)
         for (int s = 0; s < stages; s += 4) {
-            multiply_stage<BM, BN>(acc, f0, f1, buf0, buf1, buf3, at, q, s, wave, keep_last);
-            if (s + 1 < stages) multiply_stage<BM, BN>(acc, f1, f0, buf1, buf2, buf0, at, q, s + 1, wave, keep_last);
-            if (s + 2 < stages) multiply_stage<BM, BN>(acc, f0, f1, buf2, buf3, buf1, at, q, s + 2, wave, keep_last);
-            if (s + 3 < stages) multiply_stage<BM, BN>(acc, f1, f0, buf3, buf0, buf2, at, q, s + 3, wave, keep_last);
+            multiply_stage<0, BM, BN>(acc, f0, f1, sc, buf0, buf1, buf3, buf_scales, at, q, s, wave, select, keep_last, put_last);
+            if (s + 1 < stages) multiply_stage<1, BM, BN>(acc, f1, f0, sc, buf1, buf2, buf0, buf_scales, at, q, s + 1, wave, select, keep_last, put_last);
+            if (s + 2 < stages) multiply_stage<2, BM, BN>(acc, f0, f1, sc, buf2, buf3, buf1, buf_scales, at, q, s + 2, wave, select, keep_last, put_last);
+            if (s + 3 < stages) multiply_stage<3, BM, BN>(acc, f1, f0, sc, buf3, buf0, buf2, buf_scales, at, q, s + 3, wave, select, keep_last, put_last);
         }
-        __builtin_amdgcn_s_waitcnt(0x0F70);             // the empty requests too, before the LDS is another workgroup's
+        __builtin_amdgcn_s_waitcnt(0x0F70);             // the empty requests too, before the buffers are written
     }
 #pragma unroll
     for (int i = 0; i < FM; ++i)
 #pragma unroll
         for (int j = 0; j < FN; j += 4) settle(acc[i][j], acc[i][j + 1], acc[i][j + 2], acc[i][j + 3]);
-
-#pragma unroll
-    for (int i = 0; i < FM; ++i) {
-        const int64_t m = t.m0 + wm + 16 * i + row;
-        if (m >= t.m_end) continue;
-#pragma unroll
-        for (int j = 0; j < FN; ++j) {
-            const int64_t n = n0 + wn + 16 * j + 4 * part;
-            if (n < p.n) store4(p, (MODE == kMxDepth ? t.expert * p.batch_c : 0) + m * p.ldc + n, n, acc[i][j]);
-        }
-    }
+    __syncthreads();
+    uint8_t* mine = wave == 0 ? buf0 : wave == 1 ? buf1 : wave == 2 ? buf2 : buf3;
+    const int64_t base = MODE == kMxDepth ? t.expert * p.batch_c : 0;
+    store_tile<F32, FM, FN>(p, mine, acc, base, t.m0 + wm, t.m_end, n0 + wn, lane);
 }
 
 }  // namespace
 
 size_t mx_product_workspace(int64_t, int64_t, int64_t) { return 0; }
 
-template <int BM, int BN>
+template <bool F32, int BM, int BN>
 static hipError_t launch_tiles(int mode, const MxProductArgs& p, hipStream_t st) {
     const int64_t n_tiles = (p.n + BN - 1) / BN;
     int64_t m_tiles = (p.m + BM - 1) / BM;
@@ -394,17 +481,17 @@ static hipError_t launch_tiles(int mode, const MxProductArgs& p, hipStream_t st)
     const int64_t total = n_tiles * m_tiles * (mode == kMxDepth ? p.n_experts : 1);
     if (total > 0x7FFFFFFFll) return hipErrorInvalidValue;
     const dim3 grid((uint32_t)total);
-    if (mode == kMxDense) k_mx_tile<kMxDense, BM, BN><<<grid, dim3(256), 0, st>>>(p, (uint32_t)m_tiles, (uint32_t)n_tiles);
-    else if (mode == kMxRows) k_mx_tile<kMxRows, BM, BN><<<grid, dim3(256), 0, st>>>(p, (uint32_t)m_tiles, (uint32_t)n_tiles);
-    else k_mx_tile<kMxDepth, BM, BN><<<grid, dim3(256), 0, st>>>(p, (uint32_t)m_tiles, (uint32_t)n_tiles);
+    if (mode == kMxDense) k_mx_tile<kMxDense, F32, BM, BN><<<grid, dim3(256), 0, st>>>(p, (uint32_t)m_tiles, (uint32_t)n_tiles);
+    else if (mode == kMxRows) k_mx_tile<kMxRows, F32, BM, BN><<<grid, dim3(256), 0, st>>>(p, (uint32_t)m_tiles, (uint32_t)n_tiles);
+    else k_mx_tile<kMxDepth, F32, BM, BN><<<grid, dim3(256), 0, st>>>(p, (uint32_t)m_tiles, (uint32_t)n_tiles);
     return hipGetLastError();
 }
 
 hipError_t launch_mx_product(int mode, const MxProductArgs& p, void*, hipStream_t st) {
     // a tile's rows are addressed with 32-bit offsets
     const bool near = 256 * std::max(std::max(p.lda, p.ldb), std::max(p.lda_s, p.ldb_s)) < 0x7FFFFFFFll;
-    if (near && p.m > 128) return launch_tiles<256, 256>(mode, p, st);
-    if (near && p.m > 32) return launch_tiles<128, 128>(mode, p, st);
+    if (near && p.m > 128) return p.f32 ? launch_tiles<true, 256, 256>(mode, p, st) : launch_tiles<false, 256, 256>(mode, p, st);
+    if (near && p.m > 32) return p.f32 ? launch_tiles<true, 128, 128>(mode, p, st) : launch_tiles<false, 128, 128>(mode, p, st);
     const int64_t n_tiles = (p.n + kWaveN - 1) / kWaveN;
     int64_t m_tiles = (p.m + kWaveM - 1) / kWaveM;
     if (mode == kMxRows) m_tiles = p.m / kWaveM + std::min<int64_t>(p.n_experts, p.m);    // each segment ends in one part tile at most
