@@ -10,6 +10,7 @@ namespace {
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 // One v_mfma_scale_f32_16x16x128_f8f6f4 with both operands in E2M1.  Lane l holds, of operand row l % 16, the 32 codes of
 // block l / 16 (16 bytes) and that block's scale byte; of the result, rows 4 (l / 16) .. + 3 of the first operand in column
@@ -161,10 +162,14 @@ __global__ __launch_bounds__(64) void k_mx_product(MxProductArgs p, uint32_t n_t
 
 // ---- tiles through LDS -----------------------------------------------------------------------------------------------
 //
-// A workgroup of four waves forms BM x BN elements of C, each wave a quarter.  A stage is 128 of the depth, one matrix
-// instruction deep: 64 bytes of codes and 4 of scales per row, loaded from global memory straight into one of four LDS buffers.
+// A workgroup of four waves forms BM x BN elements of C, each wave a quarter.  A stage is 128 of the depth, two 32 x 32 x 64 matrix
+// instructions deep: 64 bytes of codes and 4 of scales per row, loaded from global memory straight into one of four LDS buffers.
 // While stage s is multiplied, its later fragments and the first ones of stage s + 1 are read from LDS into registers, stage
 // s + 2 is on its way and stage s + 3 is requested into the buffer that stage s - 1 left; one barrier per stage.
+//
+// One wave per SIMD (its 128 x 128 sums take half of the registers): an instruction is issued every four cycles at best, a
+// matrix instruction takes 32.  Everything else is therefore spread over the matrix instructions, a few behind each, where it
+// costs nothing; behind one another the same instructions took as long as the products.
 //
 // The four 16-byte pieces of a row lie permuted: piece j of row r at j ^ (r / 2 % 4), so that eight rows' pieces of the same
 // depth, which one LDS cycle serves, fall into different banks.  Rows beyond the operand's last lie outside the buffer
@@ -205,7 +210,7 @@ __device__ __forceinline__ void load_to_lds(uint8_t* lds, u32x4 buffer, uint32_t
 
 template <int BM, int BN>
 struct TileShape {
-    static constexpr int FM = BM / 32, FN = BN / 32;    // fragments of 16 rows of a wave
+    static constexpr int FM = BM / 64, FN = BN / 64;    // fragments of 32 rows of a wave
     static constexpr int kCodesB = BM * 64, kCodes = (BM + BN) * 64;            // bytes of a stage
     static constexpr int kScalesB = BM * 16, kScales = (BM + BN) * 16;          // bytes of four stages
     static constexpr int kRequests = kCodes / 4096, kScaleRequests = kScales / 4096;     // of one wave
@@ -220,19 +225,14 @@ struct Request {
     int last;
 };
 
-// Wave w loads the codes of rows 16 (w + 4 i) .. + 15 of one stage.
+// Wave w loads the codes of rows 16 (w + 4 i) .. + 15 of one stage: request `i` of A's, then B's.
 template <int BM, int BN>
-__device__ __forceinline__ void request_codes(uint8_t* lds, const Request& q, int stage, int wave) {
+__device__ __forceinline__ void request_codes(uint8_t* lds, const Request& q, int stage, int wave, int i) {
     typedef TileShape<BM, BN> S;
     const bool exists = stage <= q.last;
-    const u32x4 ra = q.a.at(stage * 64, exists), rb = q.b.at(stage * 64, exists);
-    const uint32_t va = stage == q.last ? q.va_last : q.va, vb = stage == q.last ? q.vb_last : q.vb;
-#pragma unroll
-    for (int i = 0; i < BM / 64; ++i)
-        load_to_lds(lds + (wave + 4 * i) * 1024, ra, va, i * q.step_a);
-#pragma unroll
-    for (int i = 0; i < BN / 64; ++i)
-        load_to_lds(lds + S::kCodesB + (wave + 4 * i) * 1024, rb, vb, i * q.step_b);
+    if (i < BM / 64) load_to_lds(lds + (wave + 4 * i) * 1024, q.a.at(stage * 64, exists), stage == q.last ? q.va_last : q.va, i * q.step_a);
+    else load_to_lds(lds + S::kCodesB + (wave + 4 * (i - BM / 64)) * 1024, q.b.at(stage * 64, exists), stage == q.last ? q.vb_last : q.vb,
+                     (i - BM / 64) * q.step_b);
 }
 // The scales of four stages, 16 bytes of a row: every row is a request of its own to the caches, so four stages share it.  Wave w
 // loads those of rows 64 w .. + 63 of either operand, or of one of them where each has 128 rows.
@@ -247,123 +247,149 @@ __device__ __forceinline__ void request_scales(uint8_t* lds, const Request& q, i
     else if (wave >= 2) load_to_lds(lds + wave * 1024, rb, q.vbs, 0);
 }
 
-// A lane's places in a buffer.
+// A lane's places in a buffer: its pieces of the two steps of a stage, its rows' scales.
 struct Place {
-    uint32_t a, b, sa, sb;              // in the codes' and the scales' buffers
+    uint32_t a[2], b[2], sa, sb;
 };
 
 template <int FN>
 struct Fragments {
-    u32x4 a0, a1, b[FN];                // the first two of A
+    u32x4 a0, a1, b[FN];                // of a step: the first two of A, all of B
 };
 template <int FM, int FN>
 struct Scales {
-    uint32_t a[FM], b[FN];              // byte t: stage t of four
+    u32x4 a[FM], b[FN];                 // word t: stage t of four; byte 0 for the first step, byte 2 for the second
 };
-template <int BM, int BN>
-__device__ __forceinline__ void read_first(Fragments<BN / 32>& f, const uint8_t* lds, const Place& at) {
+
+// The scales of this lane's row: its block of a step is 0 or 1, so the words are shifted by `half` bytes.
+__device__ __forceinline__ u32x4 own_scales(u32x4 d, uint32_t half) {
 #pragma unroll
-    for (int j = 0; j < BN / 32; ++j) f.b[j] = *reinterpret_cast<const u32x4*>(lds + at.b + j * 1024);
-    f.a0 = *reinterpret_cast<const u32x4*>(lds + at.a);
-    f.a1 = *reinterpret_cast<const u32x4*>(lds + at.a + 1024);
+    for (int t = 0; t < 4; ++t) d[t] >>= 8 * half;
+    return d;
 }
-// This lane's block of each stage: byte `part` of each of the four words; `keep` and `put` replace what lies behind the last block.
-__device__ __forceinline__ uint32_t scales_of(const uint8_t* lds, uint32_t select, uint32_t keep, uint32_t put) {
-    const u32x4 d = *reinterpret_cast<const u32x4*>(lds);
-    const uint32_t low = __builtin_amdgcn_perm(d[1], d[0], select), high = __builtin_amdgcn_perm(d[3], d[2], select);
-    return (__builtin_amdgcn_perm(high, low, 0x05040100u) & keep) | put;
-}
-
-// Four matrix instructions.  The compiler keeps the accumulators of a 128 x 128 wave in place only if told to: with the builtin it
-// gives sums and addends different registers, which do not suffice (256 of 512 are accumulators), and moves them about.  As it
-// does not look into the text, the two wait states between a vector instruction that writes an operand and a matrix instruction
-// that reads it stand there, and settle() below stands before the first other use of the sums.
-// T: which byte of the scales.
-#define MOR_MFMA(C, B, SB, SEL) "v_mfma_scale_f32_16x16x128_f8f6f4 " C ", " B ", %8, " C ", " SB ", %13 " SEL " cbsz:4 blgp:4\n\t"
-#define MOR_MFMA4(SEL)                                                                                                                    \
-    asm("s_nop 1\n\t" MOR_MFMA("%0", "%4", "%9", SEL) MOR_MFMA("%1", "%5", "%10", SEL) MOR_MFMA("%2", "%6", "%11", SEL)                    \
-            MOR_MFMA("%3", "%7", "%12", SEL)                                                                                              \
-        : "+a"(c0), "+a"(c1), "+a"(c2), "+a"(c3)                                                                                          \
-        : "v"(b0), "v"(b1), "v"(b2), "v"(b3), "v"(a), "v"(sb0), "v"(sb1), "v"(sb2), "v"(sb3), "v"(sa))
-template <int T>
-__device__ __forceinline__ void mfma4(f32x4& c0, f32x4& c1, f32x4& c2, f32x4& c3, u32x4 a, uint32_t sa, u32x4 b0, u32x4 b1, u32x4 b2, u32x4 b3,
-                                      uint32_t sb0, uint32_t sb1, uint32_t sb2, uint32_t sb3) {
-    if (T == 0) MOR_MFMA4("op_sel:[0,0,0] op_sel_hi:[0,0,0]");
-    else if (T == 1) MOR_MFMA4("op_sel:[1,1,0] op_sel_hi:[0,0,0]");
-    else if (T == 2) MOR_MFMA4("op_sel:[0,0,0] op_sel_hi:[1,1,0]");
-    else MOR_MFMA4("op_sel:[1,1,0] op_sel_hi:[1,1,0]");
-}
-#undef MOR_MFMA4
-#undef MOR_MFMA
-// The last matrix instructions (four passes of four cycles) have written their sums.
-__device__ __forceinline__ void settle(f32x4& c0, f32x4& c1, f32x4& c2, f32x4& c3) {
-    asm volatile("s_nop 15\n\ts_nop 15" : "+a"(c0), "+a"(c1), "+a"(c2), "+a"(c3));
+// The last four stages: bytes of blocks from `blocks` on (counted from the first of these stages) become 2^0.
+template <int FM, int FN>
+__device__ __forceinline__ void mask_scales(Scales<FM, FN>& s, int blocks, uint32_t half) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        uint32_t keep = 0u;
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+            if (t * 4 + b < blocks) keep |= 0xFFu << (8 * b);
+        const uint32_t put = (0x7F7F7F7Fu & ~keep) >> (8 * half);
+        keep >>= 8 * half;
+#pragma unroll
+        for (int i = 0; i < FM; ++i) s.a[i][t] = (s.a[i][t] & keep) | put;
+#pragma unroll
+        for (int j = 0; j < FN; ++j) s.b[j][t] = (s.b[j][t] & keep) | put;
+    }
 }
 
-// Stage T of four: `cur` holds its first fragments; `next` receives those of the stage in `lds_next`.  Stage 0 requests the scales
-// of the four stages after its own, stage 3 reads them.
-template <int T, int BM, int BN>
-__device__ __forceinline__ void multiply_stage(f32x4 (&acc)[BM / 32][BN / 32], Fragments<BN / 32>& cur, Fragments<BN / 32>& next,
-                                               Scales<BM / 32, BN / 32>& scales, const uint8_t* lds, const uint8_t* lds_next, uint8_t* lds_free,
-                                               uint8_t* lds_scales, const Place& at, const Request& q, int stage, int wave, uint32_t select,
-                                               uint32_t keep_last, uint32_t put_last) {
+// c += b a^T with one v_mfma_scale_f32_32x32x64_f8f6f4, both operands in E2M1: lane l holds, of operand row l % 32, the 32 codes of
+// block l / 32 and that block's scale, byte 2 STEP of a register; of the result, rows 8 (e / 4) + 4 (l / 32) + e % 4 of the first
+// operand for its elements e in column l % 32, a row of the second.
+//
+// The compiler keeps the sums of a 128 x 128 wave in place only if told to: with the builtin it gives sums and addends different
+// registers, which do not suffice (256 of 512 are sums), and moves them about.  As it does not look into the text, the two
+// wait states between a vector instruction that writes an operand and a matrix instruction that reads it stand there, and
+// settle() below stands before the first other use of the sums.
+template <int STEP>
+__device__ __forceinline__ void multiply(f32x16& c, u32x4 b, uint32_t sb, u32x4 a, uint32_t sa) {
+    if (STEP == 0)
+        asm("s_nop 1\n\tv_mfma_scale_f32_32x32x64_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[0,0,0] op_sel_hi:[0,0,0] cbsz:4 blgp:4"
+            : "+a"(c) : "v"(b), "v"(a), "v"(sb), "v"(sa));
+    else
+        asm("s_nop 1\n\tv_mfma_scale_f32_32x32x64_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[0,0,0] op_sel_hi:[1,1,0] cbsz:4 blgp:4"
+            : "+a"(c) : "v"(b), "v"(a), "v"(sb), "v"(sa));
+}
+// The last matrix instruction (eight passes of four cycles) has written its sums.
+__device__ __forceinline__ void settle(f32x16& c) { asm volatile("s_nop 15\n\ts_nop 15" : "+a"(c)); }
+
+// Half a stage, STEP of stage T of four: `cur` holds its first fragments; `next` receives those of the following step, from
+// `lds_next`.  The requests of stage `stage` + 3 are spread over both steps; stage 0 requests the scales of the four stages after its
+// own, stage 3 reads them.
+template <int T, int STEP, int BM, int BN>
+__device__ __forceinline__ void multiply_step(f32x16 (&acc)[BM / 64][BN / 64], const Fragments<BN / 64>& cur, Fragments<BN / 64>& next,
+                                              const Scales<BM / 64, BN / 64>& scales, Scales<BM / 64, BN / 64>& fresh, const uint8_t* lds,
+                                              const uint8_t* lds_next, uint8_t* lds_free, uint8_t* lds_scales, const Place& at, const Request& q,
+                                              int stage, int wave, uint32_t half) {
     typedef TileShape<BM, BN> S;
     constexpr int FM = S::FM, FN = S::FN;
-    static_assert(FM == FN, "one fragment of each operand is read per step");
-    __builtin_amdgcn_s_waitcnt(0x0F70 | (S::kRequests + (T == 1 ? S::kScaleRequests : 0)));     // all but the latest stage's requests are here
-    __syncthreads();
-    request_codes<BM, BN>(lds_free, q, stage + 3, wave);
-    if (T == 0) request_scales<BM, BN>(lds_scales, q, stage + 4, wave);
-    const bool last_four = stage + 4 >= q.last;         // (T == 3) stages s + 1 .. s + 4 hold the last one
-    const uint32_t keep = last_four ? keep_last : 0xFFFFFFFFu, put = last_four ? put_last : 0u;
+    static_assert(FM == FN, "one fragment of each operand is read per row of products");
     u32x4 a0 = cur.a0, a1 = cur.a1;
-    Scales<FM, FN> fresh;
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
         const u32x4 a = a0;
         a0 = a1;
-        a1 = *reinterpret_cast<const u32x4*>(i + 2 < FM ? lds + at.a + (i + 2) * 1024 : lds_next + at.a + (i + 2 - FM) * 1024);
-        next.b[i] = *reinterpret_cast<const u32x4*>(lds_next + at.b + i * 1024);
-        if (T == 3) {
-            fresh.a[i] = scales_of(lds_scales + at.sa + i * 256, select, keep, put);
-            fresh.b[i] = scales_of(lds_scales + at.sb + i * 256, select, keep, put);
-        }
 #pragma unroll
-        for (int j = 0; j < FN; j += 4)
-            mfma4<T>(acc[i][j], acc[i][j + 1], acc[i][j + 2], acc[i][j + 3], a, scales.a[i], cur.b[j], cur.b[j + 1], cur.b[j + 2], cur.b[j + 3],
-                     scales.b[j], scales.b[j + 1], scales.b[j + 2], scales.b[j + 3]);
-        __builtin_amdgcn_sched_barrier(0);      // the reads stay spread over the matrix instructions
+        for (int j = 0; j < FN; ++j) {
+            multiply<STEP>(acc[i][j], cur.b[j], scales.b[j][T], a, scales.a[i][T]);
+            if (j == 0)
+                a1 = *reinterpret_cast<const u32x4*>(i + 2 < FM ? lds + at.a[STEP] + (i + 2) * 2048 : lds_next + at.a[1 - STEP] + (i + 2 - FM) * 2048);
+            if (j == 1) next.b[i] = *reinterpret_cast<const u32x4*>(lds_next + at.b[1 - STEP] + i * 2048);
+            // this step's half of the requests, evenly over its products
+            constexpr int kHalf = S::kRequests / 2;
+#pragma unroll
+            for (int r = 0; r < kHalf; ++r)
+                if (i * FN + j == (r * FM * FN) / kHalf + FN / 2) request_codes<BM, BN>(lds_free, q, stage + 3, wave, STEP * kHalf + r);
+            if (T == 0 && STEP == 1 && i == FM - 1 && j == FN - 1) request_scales<BM, BN>(lds_scales, q, stage + 4, wave);
+            if (T == 3) {
+                u32x4& f = STEP == 0 ? fresh.a[i] : fresh.b[i];
+                if (j == 0) f = *reinterpret_cast<const u32x4*>(lds_scales + (STEP == 0 ? at.sa : at.sb) + i * 512);
+                if (j == FN - 1) f = own_scales(f, half);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
     }
     next.a0 = a0;
     next.a1 = a1;
-    if (T == 3) scales = fresh;
+}
+
+template <int T, int BM, int BN>
+__device__ __forceinline__ void multiply_stage(f32x16 (&acc)[BM / 64][BN / 64], Fragments<BN / 64>& f0, Fragments<BN / 64>& f1,
+                                               Scales<BM / 64, BN / 64>& scales, const uint8_t* lds, const uint8_t* lds_next, uint8_t* lds_free,
+                                               uint8_t* lds_scales, const Place& at, const Request& q, int stage, int wave, uint32_t half,
+                                               int blocks) {
+    typedef TileShape<BM, BN> S;
+    Scales<S::FM, S::FN> fresh;
+    __builtin_amdgcn_s_waitcnt(0x0F70 | (S::kRequests + (T == 1 ? S::kScaleRequests : 0)));     // all but the latest stage's requests are here
+    __syncthreads();
+    multiply_step<T, 0, BM, BN>(acc, f0, f1, scales, fresh, lds, lds, lds_free, lds_scales, at, q, stage, wave, half);
+    multiply_step<T, 1, BM, BN>(acc, f1, f0, scales, fresh, lds, lds_next, lds_free, lds_scales, at, q, stage, wave, half);
+    if (T == 3) {
+        scales = fresh;
+        if (stage + 4 >= q.last) mask_scales(scales, blocks - (stage + 1) * 4, half);
+    }
 }
 
 // A wave's sums to C by way of its LDS buffer, so that every row is written in pieces of 16 neighbouring bytes per lane: the
-// accumulators hold 4 columns of 16 rows.  `kCols` columns at a time; pieces lie permuted by the row against bank conflicts.
+// accumulators hold 4 columns of 32 rows.  `kCols` columns at a time; pieces lie permuted by the row against bank conflicts.
 template <bool F32, int FM, int FN>
-__device__ __forceinline__ void store_tile(const MxProductArgs& p, uint8_t* lds, f32x4 (&acc)[FM][FN], int64_t base, int64_t m0, int64_t m_end,
+__device__ __forceinline__ void store_tile(const MxProductArgs& p, uint8_t* lds, f32x16 (&acc)[FM][FN], int64_t base, int64_t m0, int64_t m_end,
                                            int64_t n0, int lane) {
     constexpr int kSize = F32 ? 4 : 2;
-    constexpr int kCols = FN * 16 * kSize > 256 ? 256 / kSize : FN * 16;        // a row of up to 256 bytes
+    constexpr int kCols = FN * 32 * kSize > 256 ? 256 / kSize : FN * 32;        // a row of up to 256 bytes
     constexpr int kRow = kCols * kSize, kPieces = kRow / 16, kLanes = 64 / kPieces;
-    const int row = lane & 15, part = lane >> 4;
+    const int row = lane & 31, half = lane >> 5;
 #pragma unroll
-    for (int c0 = 0; c0 < FN * 16; c0 += kCols) {
+    for (int c0 = 0; c0 < FN * 32; c0 += kCols) {
 #pragma unroll
         for (int i = 0; i < FM; ++i)
 #pragma unroll
-            for (int j = 0; j < kCols / 16; ++j) {
-                const f32x4 v = acc[i][c0 / 16 + j];
-                uint8_t* at = lds + (16 * i + row) * kRow;
-                if (F32) *reinterpret_cast<f32x4*>(at + ((4 * j + part) ^ (row & (kPieces - 1))) * 16) = v;
-                else *reinterpret_cast<u32x2*>(at + ((2 * j + (part >> 1)) ^ (row & (kPieces - 1))) * 16 + (part & 1) * 8) = narrow4(v);
-            }
+            for (int j = 0; j < kCols / 32; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const f32x16 sums = acc[i][c0 / 32 + j];
+                    const f32x4 v = {sums[4 * e], sums[4 * e + 1], sums[4 * e + 2], sums[4 * e + 3]};
+                    uint8_t* at = lds + (32 * i + row) * kRow;
+                    if (F32) *reinterpret_cast<f32x4*>(at + ((8 * j + 2 * e + half) ^ (row & (kPieces - 1))) * 16) = v;
+                    else *reinterpret_cast<u32x2*>(at + ((4 * j + e) ^ (row & (kPieces - 1))) * 16 + half * 8) = narrow4(v);
+                }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         const int piece = lane % kPieces;
         const int64_t n = n0 + c0 + piece * (16 / kSize);
 #pragma unroll 4
-        for (int r = lane / kPieces; r < FM * 16; r += kLanes) {
+        for (int r = lane / kPieces; r < FM * 32; r += kLanes) {
             const u32x4 v = *reinterpret_cast<const u32x4*>(lds + r * kRow + (piece ^ (r & (kPieces - 1))) * 16);
             if (m0 + r >= m_end || n >= p.n) break;
             uint8_t* c = reinterpret_cast<uint8_t*>(p.c) + (base + (m0 + r) * p.ldc + n) * kSize;
@@ -420,49 +446,50 @@ __global__ __launch_bounds__(256, 1) void k_mx_tile(MxProductArgs p, uint32_t m_
     q.va_last = piece_in ? q.va : kNowhere;
     q.vb_last = piece_in ? q.vb : kNowhere;
 
-    const int row = lane & 15, part = lane >> 4;
+    const int row = lane & 31;
+    const uint32_t half = lane >> 5;
     const int wm = (wave >> 1) * (BM / 2), wn = (wave & 1) * (BN / 2);
-    const uint32_t at_piece = (part ^ (row >> 1 & 3)) * 16;
-    const Place at{(uint32_t)(wm + row) * 64 + at_piece, (uint32_t)S::kCodesB + (wn + row) * 64 + at_piece, (uint32_t)(wm + row) * 16,
+    const uint32_t piece0 = (half ^ (row >> 1 & 3)) * 16, piece1 = ((half + 2) ^ (row >> 1 & 3)) * 16;
+    const uint32_t row_a = (wm + row) * 64, row_b = S::kCodesB + (wn + row) * 64;
+    const Place at{{row_a + piece0, row_a + piece1}, {row_b + piece0, row_b + piece1}, (uint32_t)(wm + row) * 16,
                    (uint32_t)S::kScalesB + (wn + row) * 16};
-    const uint32_t select = (uint32_t)part | ((uint32_t)(part + 4) << 8);
-    // the last four stages' scales: bytes of this lane's blocks that exist
-    uint32_t keep_last = 0u;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (((stages - 1) / 4 * 4 + i) * 4 + part < blocks) keep_last |= 0xFFu << (8 * i);
-    const uint32_t put_last = 0x7F7F7F7Fu & ~keep_last;
 
-    f32x4 acc[FM][FN] = {};
+    f32x16 acc[FM][FN] = {};
     if (stages > 0) {
         Fragments<FN> f0, f1;
         Scales<FM, FN> sc;
         request_scales<BM, BN>(buf_scales, q, 0, wave);
-        request_codes<BM, BN>(buf0, q, 0, wave);
-        request_codes<BM, BN>(buf1, q, 1, wave);
-        request_codes<BM, BN>(buf2, q, 2, wave);
+#pragma unroll
+        for (int i = 0; i < S::kRequests; ++i) request_codes<BM, BN>(buf0, q, 0, wave, i);
+#pragma unroll
+        for (int i = 0; i < S::kRequests; ++i) request_codes<BM, BN>(buf1, q, 1, wave, i);
+#pragma unroll
+        for (int i = 0; i < S::kRequests; ++i) request_codes<BM, BN>(buf2, q, 2, wave, i);
         __builtin_amdgcn_s_waitcnt(0x0F70 | (2 * S::kRequests & 15) | (2 * S::kRequests >> 4 << 14));
         __syncthreads();
-        read_first<BM, BN>(f0, buf0, at);
-        const uint32_t keep = stages <= 4 ? keep_last : 0xFFFFFFFFu, put = stages <= 4 ? put_last : 0u;
+        f0.a0 = *reinterpret_cast<const u32x4*>(buf0 + at.a[0]);
+        f0.a1 = *reinterpret_cast<const u32x4*>(buf0 + at.a[0] + 2048);
+#pragma unroll
+        for (int j = 0; j < FN; ++j) f0.b[j] = *reinterpret_cast<const u32x4*>(buf0 + at.b[0] + j * 2048);
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
-            sc.a[i] = scales_of(buf_scales + at.sa + i * 256, select, keep, put);
-            sc.b[i] = scales_of(buf_scales + at.sb + i * 256, select, keep, put);
+            sc.a[i] = own_scales(*reinterpret_cast<const u32x4*>(buf_scales + at.sa + i * 512), half);
+            sc.b[i] = own_scales(*reinterpret_cast<const u32x4*>(buf_scales + at.sb + i * 512), half);
         }
+        if (stages <= 4) mask_scales(sc, blocks, half);
         // (One way out of the loop: with more the compiler moves accumulators between registers.)
         for (int s = 0; s < stages; s += 4) {
-            multiply_stage<0, BM, BN>(acc, f0, f1, sc, buf0, buf1, buf3, buf_scales, at, q, s, wave, select, keep_last, put_last);
-            if (s + 1 < stages) multiply_stage<1, BM, BN>(acc, f1, f0, sc, buf1, buf2, buf0, buf_scales, at, q, s + 1, wave, select, keep_last, put_last);
-            if (s + 2 < stages) multiply_stage<2, BM, BN>(acc, f0, f1, sc, buf2, buf3, buf1, buf_scales, at, q, s + 2, wave, select, keep_last, put_last);
-            if (s + 3 < stages) multiply_stage<3, BM, BN>(acc, f1, f0, sc, buf3, buf0, buf2, buf_scales, at, q, s + 3, wave, select, keep_last, put_last);
+            multiply_stage<0, BM, BN>(acc, f0, f1, sc, buf0, buf1, buf3, buf_scales, at, q, s, wave, half, blocks);
+            if (s + 1 < stages) multiply_stage<1, BM, BN>(acc, f0, f1, sc, buf1, buf2, buf0, buf_scales, at, q, s + 1, wave, half, blocks);
+            if (s + 2 < stages) multiply_stage<2, BM, BN>(acc, f0, f1, sc, buf2, buf3, buf1, buf_scales, at, q, s + 2, wave, half, blocks);
+            if (s + 3 < stages) multiply_stage<3, BM, BN>(acc, f0, f1, sc, buf3, buf0, buf2, buf_scales, at, q, s + 3, wave, half, blocks);
         }
         __builtin_amdgcn_s_waitcnt(0x0F70);             // the empty requests too, before the buffers are written
     }
 #pragma unroll
     for (int i = 0; i < FM; ++i)
 #pragma unroll
-        for (int j = 0; j < FN; j += 4) settle(acc[i][j], acc[i][j + 1], acc[i][j + 2], acc[i][j + 3]);
+        for (int j = 0; j < FN; ++j) settle(acc[i][j]);
     __syncthreads();
     uint8_t* mine = wave == 0 ? buf0 : wave == 1 ? buf1 : wave == 2 ? buf2 : buf3;
     const int64_t base = MODE == kMxDepth ? t.expert * p.batch_c : 0;
