@@ -1,5 +1,6 @@
 // Products of microscaled 4-bit operands on the matrix cores.
 #include <algorithm>
+#include <cmath>
 
 #include "mx_device.h"
 #include "mx_launch.h"
@@ -75,6 +76,12 @@ __device__ __forceinline__ bool find_tile(const MxProductArgs& p, uint32_t m_til
     if (MODE == kMxRows) return find_rows(p, m_tile, height, tile);
     tile->m0 = (int64_t)m_tile * height;
     tile->m_end = p.m;
+    if (MODE == kMxDense && p.splits > 1) {             // z-th part of the depth, whole stages
+        const int32_t each = ((p.blocks + 7) / 8 + p.splits - 1) / p.splits * 8;
+        tile->k0 = min((int32_t)z * each, p.blocks);
+        tile->k_end = min(tile->k0 + each, p.blocks);
+        tile->expert = (int)z;
+    }
     if (MODE == kMxDepth) {
         int64_t lo, hi;
         tile->expert = (int)z;
@@ -111,7 +118,8 @@ __device__ __forceinline__ void store4(const MxProductArgs& p, int64_t at, int64
     }
 }
 
-// One wave: 32 rows of C x 64 columns, operands from global memory straight into registers.
+// One wave: 32 rows of C x 64 columns, operands from global memory straight into registers.  For operands whose rows are too far
+// apart for the kernels below.
 constexpr int kWaveM = 32, kWaveN = 64;
 template <int MODE>
 __global__ __launch_bounds__(64) void k_mx_product(MxProductArgs p, uint32_t n_tiles) {
@@ -162,20 +170,24 @@ __global__ __launch_bounds__(64) void k_mx_product(MxProductArgs p, uint32_t n_t
 
 // ---- tiles through LDS -----------------------------------------------------------------------------------------------
 //
-// A workgroup of four waves forms BM x BN elements of C, each wave a quarter.  A stage is 128 of the depth, two 32 x 32 x 64 matrix
-// instructions deep: 64 bytes of codes and 4 of scales per row, loaded from global memory straight into one of four LDS buffers.
-// While stage s is multiplied, its later fragments and the first ones of stage s + 1 are read from LDS into registers, stage
-// s + 2 is on its way and stage s + 3 is requested into the buffer that stage s - 1 left; one barrier per stage.
+// A workgroup of four waves forms BM x BN elements of C, each wave a quarter.  A stage is 256 of the depth: 128 bytes of codes and 8
+// of scales per row, loaded from global memory straight into one of two LDS buffers.  Pieces of 128 bytes matter: the L2 serves a
+// CU 57 bytes per cycle in whole lines, 30 in halves, which bound this kernel when a stage was 128 deep (8192 x 14336 x 4096:
+// 274 us).
 //
-// One wave per SIMD (its 128 x 128 sums take half of the registers): an instruction is issued every four cycles at best, a
+// A stage has four steps of 64, one 32 x 32 x 64 matrix instruction deep.  The fragments of a step are read from LDS into registers
+// while the step before is multiplied.  Those of a stage's last step are thus in registers when it begins: there is the barrier, the
+// next stage has arrived, and the one after it is requested into the buffer that is free now; it has four steps to arrive.
+//
+// With one wave per SIMD (its 128 x 128 sums take half of the registers) an instruction is issued every four cycles at best; a
 // matrix instruction takes 32.  Everything else is therefore spread over the matrix instructions, a few behind each, where it
-// costs nothing; behind one another the same instructions took as long as the products.
+// costs nothing.
 //
-// The four 16-byte pieces of a row lie permuted: piece j of row r at j ^ (r / 2 % 4), so that eight rows' pieces of the same
-// depth, which one LDS cycle serves, fall into different banks.  Rows beyond the operand's last lie outside the buffer
-// resource's range and arrive as zeros; so do the pieces behind a row's last block, whose lanes request an address out of range
-// in the last stage, and stages beyond the last, whose range is empty.  The scale bytes behind the last block, loaded four at
-// a time, are replaced by 2^0: whatever they hold, a NaN too, counts for nothing.
+// The eight 16-byte pieces of a row lie permuted: piece j of row r at j ^ (r / 2 % 8).  One LDS cycle serves 16 lanes' pieces, of
+// rows 0-3, 12-15, 20-23 and 24-27 of a fragment for example, which so fall into different banks.  Rows beyond the operand's last
+// lie outside the buffer resource's range and arrive as zeros; so do the pieces behind a row's last block, whose lanes request an
+// address out of range in the last stage, and stages beyond the last, whose range is empty.  The scale bytes behind the last
+// block, loaded 16 at a time, are replaced by 2^0: whatever they hold, a NaN too, counts for nothing.
 
 constexpr uint32_t kNowhere = 0x7FFFFFFFu;              // an offset that no range contains
 
@@ -202,18 +214,18 @@ struct RowsBuffer {
 // tracks the builtin's writes into LDS and, not being able to tell the four buffers apart across the loop, waits for all requests
 // before it reads any buffer.  Nothing is loaded into registers here, and the waits stand in multiply_stage.  (M0 is a reserved
 // register: the compiler sets it right before each use of its own, and nothing else in this kernel uses it.)
-__device__ __forceinline__ void load_to_lds(uint8_t* lds, u32x4 buffer, uint32_t offset, int group_offset) {
-    const uint32_t to = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) uint8_t*)lds);
+__device__ __forceinline__ void load_to_lds(uint32_t lds, u32x4 buffer, uint32_t offset, int group_offset) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
-                 : : "s"(to), "v"(offset), "s"(buffer), "s"(group_offset) : "memory");
+                 : : "s"(lds), "v"(offset), "s"(buffer), "s"(group_offset) : "memory");
 }
 
 template <int BM, int BN>
 struct TileShape {
     static constexpr int FM = BM / 64, FN = BN / 64;    // fragments of 32 rows of a wave
-    static constexpr int kCodesB = BM * 64, kCodes = (BM + BN) * 64;            // bytes of a stage
-    static constexpr int kScalesB = BM * 16, kScales = (BM + BN) * 16;          // bytes of four stages
-    static constexpr int kRequests = kCodes / 4096, kScaleRequests = kScales / 4096;     // of one wave
+    static constexpr int kCodesB = BM * 128, kCodes = (BM + BN) * 128;          // bytes of a stage
+    static constexpr int kScalesB = BM * 16, kScales = (BM + BN) * 16;          // bytes of two stages
+    static constexpr int kRequests = kCodes / 4096, kFirstRequests = (kRequests + 1) / 2;       // of one wave
+    static constexpr int kScalesAt = 2 * kCodes, kLds = kScalesAt + 2 * kScales;
 };
 
 // What a lane adds to the stage's base to request its pieces.
@@ -225,65 +237,65 @@ struct Request {
     int last;
 };
 
-// Wave w loads the codes of rows 16 (w + 4 i) .. + 15 of one stage: request `i` of A's, then B's.
-template <int BM, int BN>
-__device__ __forceinline__ void request_codes(uint8_t* lds, const Request& q, int stage, int wave, int i) {
-    typedef TileShape<BM, BN> S;
+// Wave w loads the codes of rows 8 (w + 4 i) .. + 7 of one stage: request `i` of A's, then B's.
+template <class S>
+__device__ __forceinline__ void request_codes(uint32_t lds, const Request& q, int stage, int wave, int i) {
+    constexpr int kOfA = S::kCodesB / 4096;
     const bool exists = stage <= q.last;
-    if (i < BM / 64) load_to_lds(lds + (wave + 4 * i) * 1024, q.a.at(stage * 64, exists), stage == q.last ? q.va_last : q.va, i * q.step_a);
-    else load_to_lds(lds + S::kCodesB + (wave + 4 * (i - BM / 64)) * 1024, q.b.at(stage * 64, exists), stage == q.last ? q.vb_last : q.vb,
-                     (i - BM / 64) * q.step_b);
+    if (i < kOfA) load_to_lds(lds + (wave + 4 * i) * 1024, q.a.at(stage * 128, exists), stage == q.last ? q.va_last : q.va, i * q.step_a);
+    else load_to_lds(lds + S::kCodesB + (wave + 4 * (i - kOfA)) * 1024, q.b.at(stage * 128, exists), stage == q.last ? q.vb_last : q.vb,
+                     (i - kOfA) * q.step_b);
 }
-// The scales of four stages, 16 bytes of a row: every row is a request of its own to the caches, so four stages share it.  Wave w
-// loads those of rows 64 w .. + 63 of either operand, or of one of them where each has 128 rows.
-template <int BM, int BN>
-__device__ __forceinline__ void request_scales(uint8_t* lds, const Request& q, int stage, int wave) {
-    typedef TileShape<BM, BN> S;
-    static_assert(BM == BN && (BM == 256 || BM == 128), "which wave loads which rows");
+// The scales of two stages, 16 bytes of a row.  Wave w loads those of rows 64 w .. + 63 of either operand; where one has fewer, several
+// waves load the same.
+template <class S>
+__device__ __forceinline__ void request_scales(uint32_t lds, const Request& q, int stage, int wave) {
     const bool exists = stage <= q.last;
-    const u32x4 ra = q.as.at(stage * 4, exists), rb = q.bs.at(stage * 4, exists);
-    if (BM == 256 || wave < 2) load_to_lds(lds + wave * 1024, ra, q.vas, 0);
-    if (BM == 256) load_to_lds(lds + S::kScalesB + wave * 1024, rb, q.vbs, 0);
-    else if (wave >= 2) load_to_lds(lds + wave * 1024, rb, q.vbs, 0);
+    load_to_lds(lds + wave % (S::kScalesB / 1024) * 1024, q.as.at(stage * 8, exists), q.vas, 0);
+    load_to_lds(lds + S::kScalesB + wave % ((S::kScales - S::kScalesB) / 1024) * 1024, q.bs.at(stage * 8, exists), q.vbs, 0);
 }
 
-// A lane's places in a buffer: its pieces of the two steps of a stage, its rows' scales.
+// A lane's places in a buffer: its pieces of the four steps of a stage, its rows' scales.
 struct Place {
-    uint32_t a[2], b[2], sa, sb;
+    uint32_t a[4], b[4], sa, sb;
 };
 
-template <int FN>
+template <int FM, int FN>
 struct Fragments {
-    u32x4 a0, a1, b[FN];                // of a step: the first two of A, all of B
+    u32x4 a[FM], b[FN];
 };
 template <int FM, int FN>
 struct Scales {
-    u32x4 a[FM], b[FN];                 // word t: stage t of four; byte 0 for the first step, byte 2 for the second
+    u32x2 a[FM], b[FN];                 // of a stage; bytes 0 and 2 of a word: two steps
 };
-
-// The scales of this lane's row: its block of a step is 0 or 1, so the words are shifted by `half` bytes.
-__device__ __forceinline__ u32x4 own_scales(u32x4 d, uint32_t half) {
-#pragma unroll
-    for (int t = 0; t < 4; ++t) d[t] >>= 8 * half;
-    return d;
-}
-// The last four stages: bytes of blocks from `blocks` on (counted from the first of these stages) become 2^0.
 template <int FM, int FN>
-__device__ __forceinline__ void mask_scales(Scales<FM, FN>& s, int blocks, uint32_t half) {
+__device__ __forceinline__ void read_fragments(Fragments<FM, FN>& f, const uint8_t* lds, const Place& at, int step) {
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-        uint32_t keep = 0u;
+    for (int i = 0; i < FM; ++i) f.a[i] = *reinterpret_cast<const u32x4*>(lds + at.a[step] + i * 4096);
 #pragma unroll
-        for (int b = 0; b < 4; ++b)
-            if (t * 4 + b < blocks) keep |= 0xFFu << (8 * b);
-        const uint32_t put = (0x7F7F7F7Fu & ~keep) >> (8 * half);
-        keep >>= 8 * half;
-#pragma unroll
-        for (int i = 0; i < FM; ++i) s.a[i][t] = (s.a[i][t] & keep) | put;
-#pragma unroll
-        for (int j = 0; j < FN; ++j) s.b[j][t] = (s.b[j][t] & keep) | put;
-    }
+    for (int j = 0; j < FN; ++j) f.b[j] = *reinterpret_cast<const u32x4*>(lds + at.b[step] + j * 4096);
 }
+
+// The scales of this lane's row: its block of a step is 0 or 1, so the words are shifted by `half` bytes; `keep` and `put` replace what
+// lies behind the last block.
+struct ScaleMask {
+    u32x2 keep, put;
+    uint32_t shift;
+    // `blocks`: those that the stage has, 8 or more: all
+    __device__ __forceinline__ ScaleMask(int blocks, uint32_t half) {
+        shift = 8 * half;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int n = min(max(blocks - 4 * t, 0), 4);
+            const uint32_t in = n == 4 ? 0xFFFFFFFFu : (1u << (8 * n)) - 1u;
+            keep[t] = in >> shift;
+            put[t] = (0x7F7F7F7Fu & ~in) >> shift;
+        }
+    }
+    __device__ __forceinline__ u32x2 operator()(u32x2 d) const {
+        return u32x2{((d[0] >> shift) & keep[0]) | put[0], ((d[1] >> shift) & keep[1]) | put[1]};
+    }
+};
 
 // c += b a^T with one v_mfma_scale_f32_32x32x64_f8f6f4, both operands in E2M1: lane l holds, of operand row l % 32, the 32 codes of
 // block l / 32 and that block's scale, byte 2 STEP of a register; of the result, rows 8 (e / 4) + 4 (l / 32) + e % 4 of the first
@@ -305,70 +317,54 @@ __device__ __forceinline__ void multiply(f32x16& c, u32x4 b, uint32_t sb, u32x4 
 // The last matrix instruction (eight passes of four cycles) has written its sums.
 __device__ __forceinline__ void settle(f32x16& c) { asm volatile("s_nop 15\n\ts_nop 15" : "+a"(c)); }
 
-// Half a stage, STEP of stage T of four: `cur` holds its first fragments; `next` receives those of the following step, from
-// `lds_next`.  The requests of stage `stage` + 3 are spread over both steps; stage 0 requests the scales of the four stages after its
-// own, stage 3 reads them.
-template <int T, int STEP, int BM, int BN>
-__device__ __forceinline__ void multiply_step(f32x16 (&acc)[BM / 64][BN / 64], const Fragments<BN / 64>& cur, Fragments<BN / 64>& next,
-                                              const Scales<BM / 64, BN / 64>& scales, Scales<BM / 64, BN / 64>& fresh, const uint8_t* lds,
-                                              const uint8_t* lds_next, uint8_t* lds_free, uint8_t* lds_scales, const Place& at, const Request& q,
-                                              int stage, int wave, uint32_t half) {
-    typedef TileShape<BM, BN> S;
-    constexpr int FM = S::FM, FN = S::FN;
-    static_assert(FM == FN, "one fragment of each operand is read per row of products");
-    u32x4 a0 = cur.a0, a1 = cur.a1;
+// Step STEP of a stage: multiplies `cur` and reads `next` from `next_a`, `next_b` (this lane's pieces there), both in slots, one behind
+// each matrix instruction.  From the last step on the requests of stage `ahead` into `to`: a CU takes one of its waves' requests
+// every 16 cycles, and a wave that has to wait with one cannot go on with its products either: half of them go into the
+// first step of the next stage (512 x 4096 x 14336: 80 us; all in the last step 88, over three steps 81, over four 92).  In the
+// last step also the scales of the next stage.
+template <int STEP, class S>
+__device__ __forceinline__ void multiply_step(f32x16 (&acc)[S::FM][S::FN], const Fragments<S::FM, S::FN>& cur, Fragments<S::FM, S::FN>& next,
+                                              const Scales<S::FM, S::FN>& scales, Scales<S::FM, S::FN>& fresh, const uint8_t* next_a,
+                                              const uint8_t* next_b, const uint8_t* scales_a, const uint8_t* scales_b, uint32_t to,
+                                              const Request& q, int ahead, int wave, const ScaleMask& mask) {
+    constexpr int FM = S::FM, FN = S::FN, kSlots = FM * FN, kWord = STEP / 2;
+    constexpr int kFirst = S::kFirstRequests, kFrom = STEP == 3 ? 0 : kFirst;
+    constexpr int kCount = STEP == 3 ? kFirst : STEP == 0 ? S::kRequests - kFirst : 0;
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
-        const u32x4 a = a0;
-        a0 = a1;
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
-            multiply<STEP>(acc[i][j], cur.b[j], scales.b[j][T], a, scales.a[i][T]);
-            if (j == 0)
-                a1 = *reinterpret_cast<const u32x4*>(i + 2 < FM ? lds + at.a[STEP] + (i + 2) * 2048 : lds_next + at.a[1 - STEP] + (i + 2 - FM) * 2048);
-            if (j == 1) next.b[i] = *reinterpret_cast<const u32x4*>(lds_next + at.b[1 - STEP] + i * 2048);
-            // this step's half of the requests, evenly over its products
-            constexpr int kHalf = S::kRequests / 2;
+            const int slot = i * FN + j;
+            multiply<STEP % 2>(acc[i][j], cur.b[j], scales.b[j][kWord], cur.a[i], scales.a[i][kWord]);
+            // the reads over the first half of the slots, so that they are complete by the end
 #pragma unroll
-            for (int r = 0; r < kHalf; ++r)
-                if (i * FN + j == (r * FM * FN) / kHalf + FN / 2) request_codes<BM, BN>(lds_free, q, stage + 3, wave, STEP * kHalf + r);
-            if (T == 0 && STEP == 1 && i == FM - 1 && j == FN - 1) request_scales<BM, BN>(lds_scales, q, stage + 4, wave);
-            if (T == 3) {
-                u32x4& f = STEP == 0 ? fresh.a[i] : fresh.b[i];
-                if (j == 0) f = *reinterpret_cast<const u32x4*>(lds_scales + (STEP == 0 ? at.sa : at.sb) + i * 512);
-                if (j == FN - 1) f = own_scales(f, half);
+            for (int r = 0; r < FM + FN; ++r)
+                if (slot == r * ((kSlots + 1) / 2) / (FM + FN)) {
+                    if (r < FN) next.b[r] = *reinterpret_cast<const u32x4*>(next_b + r * 4096);
+                    else next.a[r - FN] = *reinterpret_cast<const u32x4*>(next_a + (r - FN) * 4096);
+                }
+#pragma unroll
+            for (int r = 0; r < kCount; ++r)
+                if (slot == r * kSlots / (kCount ? kCount : 1)) request_codes<S>(to, q, ahead, wave, kFrom + r);
+            if (STEP == 3) {
+                if (j == 0) fresh.a[i] = *reinterpret_cast<const u32x2*>(scales_a + i * 512);
+                if (i == 0) fresh.b[j] = *reinterpret_cast<const u32x2*>(scales_b + j * 512);
+                if (j == FN - 1) fresh.a[i] = mask(fresh.a[i]);
+                if (i == FM - 1) fresh.b[j] = mask(fresh.b[j]);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
-    }
-    next.a0 = a0;
-    next.a1 = a1;
-}
-
-template <int T, int BM, int BN>
-__device__ __forceinline__ void multiply_stage(f32x16 (&acc)[BM / 64][BN / 64], Fragments<BN / 64>& f0, Fragments<BN / 64>& f1,
-                                               Scales<BM / 64, BN / 64>& scales, const uint8_t* lds, const uint8_t* lds_next, uint8_t* lds_free,
-                                               uint8_t* lds_scales, const Place& at, const Request& q, int stage, int wave, uint32_t half,
-                                               int blocks) {
-    typedef TileShape<BM, BN> S;
-    Scales<S::FM, S::FN> fresh;
-    __builtin_amdgcn_s_waitcnt(0x0F70 | (S::kRequests + (T == 1 ? S::kScaleRequests : 0)));     // all but the latest stage's requests are here
-    __syncthreads();
-    multiply_step<T, 0, BM, BN>(acc, f0, f1, scales, fresh, lds, lds, lds_free, lds_scales, at, q, stage, wave, half);
-    multiply_step<T, 1, BM, BN>(acc, f1, f0, scales, fresh, lds, lds_next, lds_free, lds_scales, at, q, stage, wave, half);
-    if (T == 3) {
-        scales = fresh;
-        if (stage + 4 >= q.last) mask_scales(scales, blocks - (stage + 1) * 4, half);
     }
 }
 
 // A wave's sums to C by way of its LDS buffer, so that every row is written in pieces of 16 neighbouring bytes per lane: the
 // accumulators hold 4 columns of 32 rows.  `kCols` columns at a time; pieces lie permuted by the row against bank conflicts.
-template <bool F32, int FM, int FN>
+template <bool F32, int FM, int FN, int BYTES>
 __device__ __forceinline__ void store_tile(const MxProductArgs& p, uint8_t* lds, f32x16 (&acc)[FM][FN], int64_t base, int64_t m0, int64_t m_end,
                                            int64_t n0, int lane) {
     constexpr int kSize = F32 ? 4 : 2;
-    constexpr int kCols = FN * 32 * kSize > 256 ? 256 / kSize : FN * 32;        // a row of up to 256 bytes
+    constexpr int kMost = BYTES / (FM * 32) >= 256 ? 256 : 128;                 // bytes of a row at a time
+    constexpr int kCols = FN * 32 * kSize > kMost ? kMost / kSize : FN * 32;
     constexpr int kRow = kCols * kSize, kPieces = kRow / 16, kLanes = 64 / kPieces;
     const int row = lane & 31, half = lane >> 5;
 #pragma unroll
@@ -386,33 +382,43 @@ __device__ __forceinline__ void store_tile(const MxProductArgs& p, uint8_t* lds,
                     else *reinterpret_cast<u32x2*>(at + ((4 * j + e) ^ (row & (kPieces - 1))) * 16 + half * 8) = narrow4(v);
                 }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        const int piece = lane % kPieces;
-        const int64_t n = n0 + c0 + piece * (16 / kSize);
-#pragma unroll 4
-        for (int r = lane / kPieces; r < FM * 32; r += kLanes) {
-            const u32x4 v = *reinterpret_cast<const u32x4*>(lds + r * kRow + (piece ^ (r & (kPieces - 1))) * 16);
-            if (m0 + r >= m_end || n >= p.n) break;
-            uint8_t* c = reinterpret_cast<uint8_t*>(p.c) + (base + (m0 + r) * p.ldc + n) * kSize;
-            if (n + 16 / kSize <= p.n) __builtin_memcpy(c, &v, 16);
-            else {
+        const int piece = lane % kPieces, first = lane / kPieces;
+        if (p.c_words && n0 + c0 + kCols <= p.n) {
+            // whole rows of 4-byte words: rows from `m_end` on lie outside the buffer
+            const int64_t rows = min(m_end - m0, (int64_t)FM * 32);
+            const uint32_t ld = (uint32_t)p.ldc * kSize;
+            const BufRsrc out = make_buf_window(reinterpret_cast<uint8_t*>(p.c) + (base + m0 * p.ldc + n0 + c0) * kSize,
+                                                rows > 0 ? (uint32_t)(rows - 1) * ld + kRow : 0u);
+            uint32_t at = first * ld + piece * 16;
+#pragma unroll
+            for (int r = 0; r < FM * 32; r += kLanes) {
+                const int row_r = first + r;            // its swizzle repeats: kLanes divides kPieces or the other way round
+                buf_store16<0>(out, at, *reinterpret_cast<const u32x4*>(lds + row_r * kRow + (piece ^ (row_r & (kPieces - 1))) * 16));
+                at += kLanes * ld;
+            }
+        } else {
+            const int64_t n = n0 + c0 + piece * (16 / kSize);
 #pragma unroll 1
-                for (int e = 0; n + e < p.n; ++e)       // the last columns
-                    __builtin_memcpy(c + e * kSize, lds + r * kRow + (piece ^ (r & (kPieces - 1))) * 16 + e * kSize, kSize);
+            for (int r = first; r < FM * 32; r += kLanes) {
+                if (m0 + r >= m_end || n >= p.n) break;
+                const uint8_t* v = lds + r * kRow + (piece ^ (r & (kPieces - 1))) * 16;
+                uint8_t* c = reinterpret_cast<uint8_t*>(p.c) + (base + (m0 + r) * p.ldc + n) * kSize;
+                if (n + 16 / kSize <= p.n) __builtin_memcpy(c, v, 16);
+                else {
+#pragma unroll 1
+                    for (int e = 0; n + e < p.n; ++e) __builtin_memcpy(c + e * kSize, v + e * kSize, kSize);    // the last columns
+                }
             }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
 }
 
-template <int MODE, bool F32, int BM, int BN>
-__global__ __launch_bounds__(256, 1) void k_mx_tile(MxProductArgs p, uint32_t m_tiles, uint32_t n_tiles) {
+template <int MODE, bool F32, int BM, int BN, int GROUPS>
+__global__ __launch_bounds__(256, GROUPS) void k_mx_tile(MxProductArgs p, uint32_t m_tiles, uint32_t n_tiles) {
     typedef TileShape<BM, BN> S;
     constexpr int FM = S::FM, FN = S::FN;
-    __shared__ __align__(1024) uint8_t buf0[S::kCodes];
-    __shared__ __align__(1024) uint8_t buf1[S::kCodes];
-    __shared__ __align__(1024) uint8_t buf2[S::kCodes];
-    __shared__ __align__(1024) uint8_t buf3[S::kCodes];
-    __shared__ __align__(1024) uint8_t buf_scales[S::kScales];
+    __shared__ __align__(1024) uint8_t lds[S::kLds];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // Workgroups go to the eight XCDs in turn; each XCD takes a run of tiles, in patches of 8 tile rows, so that the tiles at work
     // together share their operands in its L2.
@@ -422,7 +428,7 @@ __global__ __launch_bounds__(256, 1) void k_mx_tile(MxProductArgs p, uint32_t m_
         id = x * each + min(x, more) + id / 8;
     }
     uint32_t z = 0;
-    if (MODE == kMxDepth) { z = id / (m_tiles * n_tiles); id -= z * (m_tiles * n_tiles); }
+    if (MODE != kMxRows) { z = id / (m_tiles * n_tiles); id -= z * (m_tiles * n_tiles); }
     const uint32_t patch = id / (8 * n_tiles), in_patch = id - patch * (8 * n_tiles);
     const uint32_t tall = min(8u, m_tiles - patch * 8);
     const uint32_t m_tile = patch * 8 + in_patch % tall, n_tile = in_patch / tall;
@@ -430,59 +436,77 @@ __global__ __launch_bounds__(256, 1) void k_mx_tile(MxProductArgs p, uint32_t m_
     if (!find_tile<MODE>(p, m_tile, z, BM, &t)) return;
     const int64_t n0 = (int64_t)n_tile * BN;
     const int blocks = __builtin_amdgcn_readfirstlane(t.k_end - t.k0);
-    const int stages = (blocks + 3) / 4;
+    const int stages = (blocks + 7) / 8;
 
     const int64_t row_bytes = (int64_t)p.blocks * 16, row_scales = ((int64_t)p.blocks + 3) & ~3ll;
     const int64_t rows_a = min((int64_t)BM, t.m_end - t.m0), rows_b = min((int64_t)BN, p.n - n0);
     const int64_t of_b = MODE == kMxRows ? t.expert * p.batch_b : 0, of_bs = MODE == kMxRows ? t.expert * p.batch_bs : 0;
-    const int piece = (lane & 3) ^ (lane >> 3 & 3);     // of row lane / 4 of a group
-    const bool piece_in = (stages - 1) * 4 + piece < blocks;
+    const int piece = (lane & 7) ^ ((lane >> 4) + 4 * (wave & 1));      // of row lane / 8 of a group of 8
+    const bool piece_in = (stages - 1) * 8 + piece < blocks;
     Request q{RowsBuffer(p.a, p.lda, t.m0, rows_a, (int64_t)t.k0 * 16, row_bytes), RowsBuffer(p.as, p.lda_s, t.m0, rows_a, t.k0, row_scales),
               RowsBuffer(p.b + of_b, p.ldb, n0, rows_b, (int64_t)t.k0 * 16, row_bytes),
               RowsBuffer(p.bs + of_bs, p.ldb_s, n0, rows_b, t.k0, row_scales),
-              (uint32_t)(wave * 16 + (lane >> 2)) * (uint32_t)p.lda + piece * 16, (uint32_t)(wave * 16 + (lane >> 2)) * (uint32_t)p.ldb + piece * 16,
-              (uint32_t)(wave * 64 + lane) * (uint32_t)p.lda_s, (uint32_t)((BM == 128 ? wave - 2 : wave) * 64 + lane) * (uint32_t)p.ldb_s, 0u, 0u,
-              (int)p.lda * 64, (int)p.ldb * 64, stages - 1};
+              (uint32_t)(wave * 8 + (lane >> 3)) * (uint32_t)p.lda + piece * 16, (uint32_t)(wave * 8 + (lane >> 3)) * (uint32_t)p.ldb + piece * 16,
+              (uint32_t)(wave % (BM / 64) * 64 + lane) * (uint32_t)p.lda_s, (uint32_t)(wave % (BN / 64) * 64 + lane) * (uint32_t)p.ldb_s, 0u, 0u,
+              (int)p.lda * 32, (int)p.ldb * 32, stages - 1};
     q.va_last = piece_in ? q.va : kNowhere;
     q.vb_last = piece_in ? q.vb : kNowhere;
 
     const int row = lane & 31;
     const uint32_t half = lane >> 5;
     const int wm = (wave >> 1) * (BM / 2), wn = (wave & 1) * (BN / 2);
-    const uint32_t piece0 = (half ^ (row >> 1 & 3)) * 16, piece1 = ((half + 2) ^ (row >> 1 & 3)) * 16;
-    const uint32_t row_a = (wm + row) * 64, row_b = S::kCodesB + (wn + row) * 64;
-    const Place at{{row_a + piece0, row_a + piece1}, {row_b + piece0, row_b + piece1}, (uint32_t)(wm + row) * 16,
-                   (uint32_t)S::kScalesB + (wn + row) * 16};
+    Place at;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        const uint32_t at_piece = ((2 * t + half) ^ (row >> 1 & 7)) * 16;
+        at.a[t] = (wm + row) * 128 + at_piece;
+        at.b[t] = S::kCodesB + (wn + row) * 128 + at_piece;
+    }
+    at.sa = (wm + row) * 16;
+    at.sb = S::kScalesB + (wn + row) * 16;
 
-    f32x16 acc[FM][FN] = {};
+    f32x16 acc[FM][FN];
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[i][j] = f32x16{};
     if (stages > 0) {
-        Fragments<FN> f0, f1;
+        Fragments<FM, FN> f0, f1;
         Scales<FM, FN> sc;
-        request_scales<BM, BN>(buf_scales, q, 0, wave);
+        const uint32_t lds_at = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) uint8_t*)lds);
+        const uint8_t* lds_scales = lds + S::kScalesAt;
+        request_scales<S>(lds_at + S::kScalesAt, q, 0, wave);
 #pragma unroll
-        for (int i = 0; i < S::kRequests; ++i) request_codes<BM, BN>(buf0, q, 0, wave, i);
+        for (int i = 0; i < S::kRequests; ++i) request_codes<S>(lds_at, q, 0, wave, i);
 #pragma unroll
-        for (int i = 0; i < S::kRequests; ++i) request_codes<BM, BN>(buf1, q, 1, wave, i);
-#pragma unroll
-        for (int i = 0; i < S::kRequests; ++i) request_codes<BM, BN>(buf2, q, 2, wave, i);
-        __builtin_amdgcn_s_waitcnt(0x0F70 | (2 * S::kRequests & 15) | (2 * S::kRequests >> 4 << 14));
+        for (int i = 0; i < S::kFirstRequests; ++i) request_codes<S>(lds_at + S::kCodes, q, 1, wave, i);
+        __builtin_amdgcn_s_waitcnt(0x0F70 | S::kFirstRequests);
         __syncthreads();
-        f0.a0 = *reinterpret_cast<const u32x4*>(buf0 + at.a[0]);
-        f0.a1 = *reinterpret_cast<const u32x4*>(buf0 + at.a[0] + 2048);
+        read_fragments(f0, lds, at, 0);
+        {
+            const ScaleMask mask(blocks, half);
 #pragma unroll
-        for (int j = 0; j < FN; ++j) f0.b[j] = *reinterpret_cast<const u32x4*>(buf0 + at.b[0] + j * 2048);
+            for (int i = 0; i < FM; ++i) sc.a[i] = mask(*reinterpret_cast<const u32x2*>(lds_scales + at.sa + i * 512));
 #pragma unroll
-        for (int i = 0; i < FM; ++i) {
-            sc.a[i] = own_scales(*reinterpret_cast<const u32x4*>(buf_scales + at.sa + i * 512), half);
-            sc.b[i] = own_scales(*reinterpret_cast<const u32x4*>(buf_scales + at.sb + i * 512), half);
+            for (int j = 0; j < FN; ++j) sc.b[j] = mask(*reinterpret_cast<const u32x2*>(lds_scales + at.sb + j * 512));
         }
-        if (stages <= 4) mask_scales(sc, blocks, half);
-        // (One way out of the loop: with more the compiler moves accumulators between registers.)
-        for (int s = 0; s < stages; s += 4) {
-            multiply_stage<0, BM, BN>(acc, f0, f1, sc, buf0, buf1, buf3, buf_scales, at, q, s, wave, half, blocks);
-            if (s + 1 < stages) multiply_stage<1, BM, BN>(acc, f0, f1, sc, buf1, buf2, buf0, buf_scales, at, q, s + 1, wave, half, blocks);
-            if (s + 2 < stages) multiply_stage<2, BM, BN>(acc, f0, f1, sc, buf2, buf3, buf1, buf_scales, at, q, s + 2, wave, half, blocks);
-            if (s + 3 < stages) multiply_stage<3, BM, BN>(acc, f0, f1, sc, buf3, buf0, buf2, buf_scales, at, q, s + 3, wave, half, blocks);
+        uint32_t cur = 0u;                              // buffer of the stage
+        for (int s = 0; s < stages; ++s) {
+            const uint8_t *here = lds + cur, *there = lds + (S::kCodes - cur);
+            // the next stage's scales: pairs of stages take turns in two buffers
+            const uint8_t* sc_next = lds_scales + ((s + 1) >> 1 & 1) * S::kScales + ((s + 1) & 1) * 8;
+            const uint32_t to_here = lds_at + cur, to_there = lds_at + (S::kCodes - cur);
+            const ScaleMask mask(blocks - (s + 1) * 8, half);
+            Scales<FM, FN> fresh;
+            multiply_step<0, S>(acc, f0, f1, sc, fresh, here + at.a[1], here + at.b[1], sc_next + at.sa, sc_next + at.sb, to_there, q, s + 1, wave, mask);
+            multiply_step<1, S>(acc, f1, f0, sc, fresh, here + at.a[2], here + at.b[2], sc_next + at.sa, sc_next + at.sb, to_there, q, s + 1, wave, mask);
+            multiply_step<2, S>(acc, f0, f1, sc, fresh, here + at.a[3], here + at.b[3], sc_next + at.sa, sc_next + at.sb, to_there, q, s + 1, wave, mask);
+            __builtin_amdgcn_s_waitcnt(0x0070);         // this wave's reads of the stage are complete, its requests of the next one too
+            __syncthreads();
+            if ((s & 1) == 0) request_scales<S>(lds_at + S::kScalesAt + ((s >> 1) + 1 & 1) * S::kScales, q, s + 2, wave);
+            multiply_step<3, S>(acc, f1, f0, sc, fresh, there + at.a[0], there + at.b[0], sc_next + at.sa, sc_next + at.sb, to_here, q, s + 2, wave, mask);
+            sc = fresh;
+            cur = S::kCodes - cur;
         }
         __builtin_amdgcn_s_waitcnt(0x0F70);             // the empty requests too, before the buffers are written
     }
@@ -491,34 +515,202 @@ __global__ __launch_bounds__(256, 1) void k_mx_tile(MxProductArgs p, uint32_t m_
 #pragma unroll
         for (int j = 0; j < FN; ++j) settle(acc[i][j]);
     __syncthreads();
-    uint8_t* mine = wave == 0 ? buf0 : wave == 1 ? buf1 : wave == 2 ? buf2 : buf3;
-    const int64_t base = MODE == kMxDepth ? t.expert * p.batch_c : 0;
-    store_tile<F32, FM, FN>(p, mine, acc, base, t.m0 + wm, t.m_end, n0 + wn, lane);
+    constexpr int kShare = S::kLds / 4 & ~1023;
+    uint8_t* mine = lds + wave * kShare;
+    const int64_t base = MODE != kMxRows ? t.expert * p.batch_c : 0;
+    store_tile<F32, FM, FN, kShare>(p, mine, acc, base, t.m0 + wm, t.m_end, n0 + wn, lane);
+}
+
+// ---- few rows ---------------------------------------------------------------------------------------------------------
+//
+// Up to 64 rows of A (tokens) against all of B (weights): what counts is how fast B's bytes come in.  Eight waves share a
+// workgroup's 16 NT rows of B and split the depth between them, in groups of 512 (four matrix instructions); every wave has a
+// group's loads on their way at once, straight into registers.  The partial sums are joined through LDS, in the order of the waves.
+constexpr int kFewWaves = 8;
+template <int MODE, int MT, int NT>
+__global__ __launch_bounds__(kFewWaves * 64) void k_mx_few(MxProductArgs p, uint32_t n_tiles) {
+    __shared__ __align__(16) f32x4 sums[kFewWaves][MT * NT][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t n_tile = blockIdx.x % n_tiles, m_tile = blockIdx.x / n_tiles;
+    Tile t;
+    if (!find_tile<MODE>(p, m_tile, blockIdx.z, 16 * MT, &t)) return;
+    const int64_t n0 = (int64_t)n_tile * (16 * NT);
+    const int64_t row_bytes = (int64_t)p.blocks * 16, row_scales = ((int64_t)p.blocks + 3) & ~3ll;
+    const int64_t rows_a = min((int64_t)(16 * MT), t.m_end - t.m0), rows_b = min((int64_t)(16 * NT), p.n - n0);
+    const RowsBuffer a(p.a, p.lda, t.m0, rows_a, 0, row_bytes), as(p.as, p.lda_s, t.m0, rows_a, 0, row_scales);
+    const RowsBuffer b(p.b + (MODE == kMxRows ? t.expert * p.batch_b : 0), p.ldb, n0, rows_b, 0, row_bytes);
+    const RowsBuffer bs(p.bs + (MODE == kMxRows ? t.expert * p.batch_bs : 0), p.ldb_s, n0, rows_b, 0, row_scales);
+    const BufRsrc ra = make_buf_window(a.base, a.bytes), ras = make_buf_window(as.base, as.bytes);
+    const BufRsrc rb = make_buf_window(b.base, b.bytes), rbs = make_buf_window(bs.base, bs.bytes);
+    const int row = lane & 15, part = lane >> 4;
+    f32x4 acc[MT][NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{};
+    const int groups = (p.blocks + 15) / 16;
+    for (int g = wave; g < groups; g += kFewWaves) {
+        u32x4 av[MT][4], bv[NT][4], sa[MT], sb[NT];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+                bv[j][s] = __builtin_amdgcn_raw_buffer_load_b128(rb, (uint32_t)(16 * j + row) * (uint32_t)p.ldb + part * 16 + s * 64, g * 256, 0);
+            sb[j] = __builtin_amdgcn_raw_buffer_load_b128(rbs, (uint32_t)(16 * j + row) * (uint32_t)p.ldb_s, g * 16, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+                av[i][s] = __builtin_amdgcn_raw_buffer_load_b128(ra, (uint32_t)(16 * i + row) * (uint32_t)p.lda + part * 16 + s * 64, g * 256, 0);
+            sa[i] = __builtin_amdgcn_raw_buffer_load_b128(ras, (uint32_t)(16 * i + row) * (uint32_t)p.lda_s, g * 16, 0);
+        }
+        const bool ragged = g * 16 + 16 > p.blocks;
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            const bool in = !ragged || g * 16 + s * 4 + part < p.blocks;        // behind the last block: codes 0, scales 2^0
+            uint32_t scale_b[NT];
+#pragma unroll
+            for (int j = 0; j < NT; ++j) scale_b[j] = in ? sb[j][s] >> (8 * part) : 127u;
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                const u32x4 codes = in ? av[i][s] : u32x4{0u, 0u, 0u, 0u};
+                const uint32_t scale_a = in ? sa[i][s] >> (8 * part) : 127u;
+#pragma unroll
+                for (int j = 0; j < NT; ++j) acc[i][j] = mfma_mx(bv[j][s], scale_b[j], codes, scale_a, acc[i][j]);
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) sums[wave][i * NT + j][lane] = acc[i][j];
+    __syncthreads();
+    for (int f = wave; f < MT * NT; f += kFewWaves) {
+        f32x4 v = sums[0][f][lane];
+#pragma unroll
+        for (int w = 1; w < kFewWaves; ++w) {
+            const f32x4 u = sums[w][f][lane];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += u[e];
+        }
+        const int64_t m = t.m0 + f / NT * 16 + row, n = n0 + f % NT * 16 + 4 * part;
+        if (m < t.m_end && n < p.n) store4(p, m * p.ldc + n, n, v);
+    }
+}
+
+// Joins the parts of a split depth, in their order: four elements of a row per lane.
+__global__ __launch_bounds__(256) void k_mx_join(MxProductArgs p, const float* parts, int64_t ld, int64_t batch, int splits) {
+    const int64_t per_row = ld / 4, i = (int64_t)blockIdx.x * 256 + threadIdx.x, m = i / per_row, n = (i - m * per_row) * 4;
+    if (m >= p.m || n >= p.n) return;
+    f32x4 v = *reinterpret_cast<const f32x4*>(parts + m * ld + n);
+    for (int s = 1; s < splits; ++s) {
+        const f32x4 u = *reinterpret_cast<const f32x4*>(parts + s * batch + m * ld + n);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += u[e];
+    }
+    store4(p, m * p.ldc + n, n, v);
 }
 
 }  // namespace
 
-size_t mx_product_workspace(int64_t, int64_t, int64_t) { return 0; }
+// Which kernel a product of a given size takes.  Times in us, measured on whole and partly filled cards: a stage of a 256 x 256 tile
+// 1.9, of two 128 x 128 tiles on a CU 1.29, of one 0.56, and what a tile costs besides 8 and 5.  (8192 x 14336 x 4096: 263 us in
+// large tiles, 322 in small ones; 2048 x 2048 x 2048: 20.4 and 10.3.)
+struct ProductPlan {
+    enum { kFew, kSmallTiles, kLargeTiles } kind;
+    int splits;                         // parts of the depth
+};
+static ProductPlan plan_product(int mode, int64_t m, int64_t n, int64_t blocks, int64_t experts) {
+    if (mode == kMxDense && m <= 64) return {ProductPlan::kFew, 1};
+    if (mode == kMxRows && m <= 32 * experts) return {ProductPlan::kFew, 1};
+    const double stages = (double)((blocks + 7) / 8);
+    const int64_t batch = mode == kMxDepth ? experts : 1;
+    const int64_t large = ((m + 255) / 256) * ((n + 255) / 256) * batch, small = ((m + 127) / 128) * ((n + 127) / 128) * batch;
+    const int64_t rest = small % 512;
+    const double in_large = (double)((large + 255) / 256) * (1.9 * stages + 8);
+    const double in_small = (double)(small / 512) * (1.29 * stages + 5) + (rest == 0 ? 0.0 : (rest <= 256 ? 0.56 : 1.29) * stages + 5);
+    if (in_large <= in_small) return {ProductPlan::kLargeTiles, 1};
+    // Few tiles and a long depth: parts of it on idle CUs.  They are written and read again at about 4 TB/s, and joining them is a
+    // launch of its own (128 x 4096 x 14336: 18.5 us in eight parts, 42 in one; 512 x 4096 x 4096: 18.2 in two, 13.9 in one).
+    ProductPlan best{ProductPlan::kSmallTiles, 1};
+    double least = in_small;
+    if (mode == kMxDense && small <= 128)
+        for (int splits = 2; splits * small <= 256 && splits <= 32; splits *= 2) {
+            const double time = std::ceil(stages / splits) * 0.56 + 9 + (double)splits * (double)m * (double)n * 8e-6 / 4;
+            if (time < least) { least = time; best.splits = splits; }
+        }
+    return best;
+}
+static int64_t part_ld(int64_t n) { return (n + 3) / 4 * 4; }
 
-template <bool F32, int BM, int BN>
+size_t mx_product_workspace(int64_t m, int64_t n, int64_t blocks) {
+    const int splits = plan_product(kMxDense, m, n, blocks, 1).splits;
+    return splits == 1 ? 0 : (size_t)splits * m * part_ld(n) * 4;
+}
+
+template <bool F32, int BM, int BN, int GROUPS>
 static hipError_t launch_tiles(int mode, const MxProductArgs& p, hipStream_t st) {
     const int64_t n_tiles = (p.n + BN - 1) / BN;
     int64_t m_tiles = (p.m + BM - 1) / BM;
     if (mode == kMxRows) m_tiles = p.m / BM + std::min<int64_t>(p.n_experts, p.m);
-    const int64_t total = n_tiles * m_tiles * (mode == kMxDepth ? p.n_experts : 1);
+    const int64_t total = n_tiles * m_tiles * (mode == kMxDepth ? p.n_experts : p.splits);
     if (total > 0x7FFFFFFFll) return hipErrorInvalidValue;
     const dim3 grid((uint32_t)total);
-    if (mode == kMxDense) k_mx_tile<kMxDense, F32, BM, BN><<<grid, dim3(256), 0, st>>>(p, (uint32_t)m_tiles, (uint32_t)n_tiles);
-    else if (mode == kMxRows) k_mx_tile<kMxRows, F32, BM, BN><<<grid, dim3(256), 0, st>>>(p, (uint32_t)m_tiles, (uint32_t)n_tiles);
-    else k_mx_tile<kMxDepth, F32, BM, BN><<<grid, dim3(256), 0, st>>>(p, (uint32_t)m_tiles, (uint32_t)n_tiles);
+    if (mode == kMxDense) k_mx_tile<kMxDense, F32, BM, BN, GROUPS><<<grid, dim3(256), 0, st>>>(p, (uint32_t)m_tiles, (uint32_t)n_tiles);
+    else if (mode == kMxRows) k_mx_tile<kMxRows, F32, BM, BN, GROUPS><<<grid, dim3(256), 0, st>>>(p, (uint32_t)m_tiles, (uint32_t)n_tiles);
+    else k_mx_tile<kMxDepth, F32, BM, BN, GROUPS><<<grid, dim3(256), 0, st>>>(p, (uint32_t)m_tiles, (uint32_t)n_tiles);
     return hipGetLastError();
 }
 
-hipError_t launch_mx_product(int mode, const MxProductArgs& p, void*, hipStream_t st) {
-    // a tile's rows are addressed with 32-bit offsets
-    const bool near = 256 * std::max(std::max(p.lda, p.ldb), std::max(p.lda_s, p.ldb_s)) < 0x7FFFFFFFll;
-    if (near && p.m > 128) return p.f32 ? launch_tiles<true, 256, 256>(mode, p, st) : launch_tiles<false, 256, 256>(mode, p, st);
-    if (near && p.m > 32) return p.f32 ? launch_tiles<true, 128, 128>(mode, p, st) : launch_tiles<false, 128, 128>(mode, p, st);
+template <int MT, int NT>
+static hipError_t launch_few(int mode, const MxProductArgs& p, hipStream_t st) {
+    const int64_t n_tiles = (p.n + 16 * NT - 1) / (16 * NT);
+    int64_t m_tiles = (p.m + 16 * MT - 1) / (16 * MT);
+    if (mode == kMxRows) m_tiles = p.m / (16 * MT) + std::min<int64_t>(p.n_experts, p.m);
+    if (n_tiles * m_tiles > 0x7FFFFFFFll) return hipErrorInvalidValue;
+    const dim3 grid((uint32_t)(n_tiles * m_tiles)), block(kFewWaves * 64);
+    if (mode == kMxDense) k_mx_few<kMxDense, MT, NT><<<grid, block, 0, st>>>(p, (uint32_t)n_tiles);
+    else k_mx_few<kMxRows, MT, NT><<<grid, block, 0, st>>>(p, (uint32_t)n_tiles);
+    return hipGetLastError();
+}
+
+static bool near_rows(const MxProductArgs& p) {         // 256 rows of either operand within 32-bit offsets
+    return 256 * std::max(std::max(p.lda, p.ldb), std::max(p.lda_s, p.ldb_s)) < 0x7FFFFFFFll;
+}
+static hipError_t launch_all_tiles(int mode, MxProductArgs p, bool large, hipStream_t st) {
+    const int64_t size = p.f32 ? 4 : 2;
+    p.c_words = ((reinterpret_cast<uintptr_t>(p.c) | (uintptr_t)(p.ldc * size) | (uintptr_t)(p.batch_c * size)) & 3) == 0 && 256 * p.ldc * size < 0x7FFFFFFFll;
+    if (large) return p.f32 ? launch_tiles<true, 256, 256, 1>(mode, p, st) : launch_tiles<false, 256, 256, 1>(mode, p, st);
+    return p.f32 ? launch_tiles<true, 128, 128, 2>(mode, p, st) : launch_tiles<false, 128, 128, 2>(mode, p, st);
+}
+
+hipError_t launch_mx_product(int mode, MxProductArgs p, void* workspace, hipStream_t st) {
+    p.splits = 1;
+    if (near_rows(p)) {
+        const ProductPlan plan = plan_product(mode, p.m, p.n, p.blocks, p.n_experts);
+        if (plan.kind == ProductPlan::kFew) {
+            // twice the rows of B per workgroup where that leaves enough workgroups: A's rows are read half as often
+            const bool wide = p.n > 8192;
+            if (mode == kMxRows || p.m <= 4) return launch_few<1, 1>(mode, p, st);
+            if (p.m <= 16) return wide ? launch_few<1, 2>(mode, p, st) : launch_few<1, 1>(mode, p, st);
+            if (p.m <= 32) return wide ? launch_few<2, 2>(mode, p, st) : launch_few<2, 1>(mode, p, st);
+            return wide ? launch_few<4, 2>(mode, p, st) : launch_few<4, 1>(mode, p, st);
+        }
+        if (plan.splits == 1) return launch_all_tiles(mode, p, plan.kind == ProductPlan::kLargeTiles, st);
+        MxProductArgs part = p;
+        part.c = workspace;
+        part.ldc = part_ld(p.n);
+        part.batch_c = p.m * part.ldc;
+        part.f32 = 1;
+        part.splits = plan.splits;
+        const hipError_t e = launch_all_tiles(mode, part, false, st);
+        if (e != hipSuccess) return e;
+        const int64_t lanes = p.m * (part.ldc / 4);
+        const dim3 grid((uint32_t)((lanes + 255) / 256));
+        k_mx_join<<<grid, dim3(256), 0, st>>>(p, static_cast<const float*>(workspace), part.ldc, part.batch_c, plan.splits);
+        return hipGetLastError();
+    }
     const int64_t n_tiles = (p.n + kWaveN - 1) / kWaveN;
     int64_t m_tiles = (p.m + kWaveM - 1) / kWaveM;
     if (mode == kMxRows) m_tiles = p.m / kWaveM + std::min<int64_t>(p.n_experts, p.m);    // each segment ends in one part tile at most

@@ -199,7 +199,9 @@ def product(a, b, dtype, **kw):
 
 PRODUCTS = [(1, 1, 1), (1, 16, 32), (1, 300, 4096), (2, 17, 33), (5, 1000, 1500), (16, 64, 128), (17, 128, 160), (33, 65, 127), (64, 512, 256),
             (100, 40, 5000), (128, 128, 128), (129, 257, 513), (200, 1, 640), (256, 256, 256), (257, 512, 1024), (300, 400, 4130),
-            (512, 768, 2048), (1000, 130, 96), (2100, 2050, 300)]
+            (512, 768, 2048), (1000, 130, 96), (2100, 2050, 300),
+            # parts of the depth on different workgroups, the last one shorter, and a result joined from them
+            (70, 100, 4096), (100, 257, 8200), (300, 130, 6000)]
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
