@@ -29,13 +29,14 @@ __device__ __forceinline__ float mx_scale_inverse(uint32_t byte) { return __uint
 
 // Philox 4 x 32 (J. Salmon, M. Moraes, R. Dror, D. Shaw: "Parallel random numbers: as easy as 1, 2, 3", 2011) with seven
 // rounds, the fewest for which the authors report that every statistical test passes; ten cost 1.4 times as much.
+__device__ __forceinline__ uint32_t xor3(uint32_t a, uint32_t b, uint32_t c) { return __builtin_amdgcn_bitop3_b32(a, b, c, 0x96); }
 __device__ __forceinline__ u32x4 philox(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3, uint32_t k0, uint32_t k1) {
 #pragma unroll
     for (int i = 0; i < 7; ++i) {
         const uint64_t p0 = (uint64_t)c0 * 0xD2511F53u, p1 = (uint64_t)c2 * 0xCD9E8D57u;
-        c0 = (uint32_t)(p1 >> 32) ^ c1 ^ k0;
+        c0 = xor3((uint32_t)(p1 >> 32), c1, k0);
         c1 = (uint32_t)p1;
-        c2 = (uint32_t)(p0 >> 32) ^ c3 ^ k1;
+        c2 = xor3((uint32_t)(p0 >> 32), c3, k1);
         c3 = (uint32_t)p0;
         k0 += 0x9E3779B9u;
         k1 += 0xBB67AE85u;
@@ -43,13 +44,16 @@ __device__ __forceinline__ u32x4 philox(uint32_t c0, uint32_t c1, uint32_t c2, u
     return u32x4{c0, c1, c2, c3};
 }
 
-// Stochastic code of one value: v = element in binary32, inv = 2^-e, r = 16 random bits.
-__device__ __forceinline__ uint32_t mx_code_stochastic(float v, float inv, uint32_t r) {
-    const float y = __builtin_fabsf(v) * inv;
-    const float per_step = y < 2.0f ? 2.0f : (y < 4.0f ? 1.0f : 0.5f);
-    const uint32_t first = y < 2.0f ? 0u : (y < 4.0f ? 2u : 4u);    // code minus multiple of the step
-    const uint32_t code = min((uint32_t)(y * per_step + (float)r * 0x1p-16f) + first, 7u);
-    return code | ((__float_as_uint(v) >> 31) << 3);
+// Stochastic code of one magnitude, not yet less kStochasticBase and not yet with its sign: v = element in binary32, shift = 23 - e, r = 16
+// random bits.  From 1 on a grid value has one mantissa bit, so y = |v| 2^-e rounds up where the 22 bits behind it, plus r 2^6,
+// carry: bit 22 of y's pattern on is the code (plus a constant).  Below 1 the same holds of y 2^23 as a whole number, whose
+// steps are those of the binade below 2.  Whole numbers throughout: floor(y / step + r / 65536) without a rounding of its own.
+constexpr uint32_t kStochasticBase = 2 * (127 - 1) + 2 * 23;
+__device__ __forceinline__ uint32_t mx_code_stochastic(float v, int shift, uint32_t r) {
+    const float y = __builtin_amdgcn_ldexpf(__builtin_fabsf(v), shift);     // y 2^23
+    const uint32_t whole = (uint32_t)y + (kStochasticBase << 22);
+    const uint32_t w = (y < 0x1p23f ? whole : __float_as_uint(y)) + (r << 6);
+    return min(w >> 22, kStochasticBase + 7u);
 }
 
 __device__ __forceinline__ bf16x2 bf16_pair(uint32_t word) { return __builtin_bit_cast(bf16x2, word); }
@@ -74,14 +78,17 @@ __device__ __forceinline__ uint32_t mx_codes8_nearest(const float (&v)[8], uint3
     return byte == kMxNan ? 0u : c;
 }
 __device__ __forceinline__ uint32_t mx_codes8_stochastic(const float (&v)[8], uint32_t byte, const u32x4& random) {
-    const float inv = mx_scale_inverse(byte);
-    uint32_t c = 0;
+    const int shift = 23 + 127 - (int)byte;
+    uint32_t c = 0u - kStochasticBase * 0x11111111u, sign = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        c |= mx_code_stochastic(v[2 * j], inv, random[j] & 0xFFFFu) << (8 * j);
-        c |= mx_code_stochastic(v[2 * j + 1], inv, random[j] >> 16) << (8 * j + 4);
+        const uint32_t word = random[j];
+        c += mx_code_stochastic(v[2 * j], shift, word & 0xFFFFu) << (8 * j);
+        c += mx_code_stochastic(v[2 * j + 1], shift, word >> 16) << (8 * j + 4);
+        sign |= (__float_as_uint(v[2 * j]) >> 31) << (8 * j + 3);
+        sign |= (__float_as_uint(v[2 * j + 1]) >> 31) << (8 * j + 7);
     }
-    return byte == kMxNan ? 0u : c;
+    return byte == kMxNan ? 0u : c | sign;
 }
 __device__ __forceinline__ void widen8(const u32x4& raw, float (&v)[8]) {
 #pragma unroll
@@ -94,15 +101,26 @@ __device__ __forceinline__ void widen8(const u32x4& raw, float (&v)[8]) {
 
 // Eight elements of a BF16 row from column c on; the last ones of a row may be missing and read as zeros.  Rows may start at any
 // element: the wide accesses need no more than the elements' own alignment.
+typedef u32x4 u32x4_anywhere __attribute__((aligned(2)));
+template <bool STREAM = false>
 __device__ __forceinline__ u32x4 load8(const uint16_t* row, int64_t c, int64_t cols) {
+    if (c + 8 <= cols) {
+        const u32x4_anywhere* p = reinterpret_cast<const u32x4_anywhere*>(row + c);
+        return STREAM ? __builtin_nontemporal_load(p) : *p;
+    }
     u32x4 v{0u, 0u, 0u, 0u};
-    if (c + 8 <= cols) { __builtin_memcpy(&v, row + c, 16); return v; }
     for (int j = 0; j < 8; ++j)
         if (c + j < cols) v[j >> 1] |= (uint32_t)row[c + j] << (16 * (j & 1));
     return v;
 }
+template <bool STREAM = false>
 __device__ __forceinline__ void store8(uint16_t* row, int64_t c, int64_t cols, const u32x4& v) {
-    if (c + 8 <= cols) { __builtin_memcpy(row + c, &v, 16); return; }
+    if (c + 8 <= cols) {
+        u32x4_anywhere* p = reinterpret_cast<u32x4_anywhere*>(row + c);
+        if (STREAM) __builtin_nontemporal_store(v, p);
+        else *p = v;
+        return;
+    }
     for (int j = 0; j < 8; ++j)
         if (c + j < cols) row[c + j] = (uint16_t)(v[j >> 1] >> (16 * (j & 1)));
 }

@@ -132,6 +132,7 @@ __device__ __forceinline__ u32x4 narrow8(const float (&f)[8]) {
 
 constexpr int kRowSpan = 1024;          // elements of a row that one wave moves: two chunks per lane
 
+template <bool STREAM>
 __global__ __launch_bounds__(256) void k_expert_gather(const uint16_t* x, int64_t ld_x, int64_t d, MxOrder o, uint16_t* xs, int64_t ld_xs) {
     const int64_t slot = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (slot >= o.capacity) return;
@@ -140,11 +141,11 @@ __global__ __launch_bounds__(256) void k_expert_gather(const uint16_t* x, int64_
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const int64_t c = (int64_t)blockIdx.y * kRowSpan + h * 512 + (threadIdx.x & 63) * 8;
-        if (c < d) store8(xs + slot * ld_xs, c, d, row ? load8(row, c, d) : u32x4{0u, 0u, 0u, 0u});
+        if (c < d) store8<STREAM>(xs + slot * ld_xs, c, d, row ? load8(row, c, d) : u32x4{0u, 0u, 0u, 0u});
     }
 }
 
-template <bool WEIGHTS>
+template <bool WEIGHTS, bool STREAM>
 __global__ __launch_bounds__(256) void k_expert_combine(const uint16_t* ys, int64_t ld_ys, int64_t d, MxOrder o, const float* weights,
                                                         uint16_t* y, int64_t ld_y) {
     const int64_t token = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -160,7 +161,7 @@ __global__ __launch_bounds__(256) void k_expert_combine(const uint16_t* ys, int6
             const int64_t c = (int64_t)blockIdx.y * kRowSpan + h * 512 + (threadIdx.x & 63) * 8;
             if (c >= d) continue;
             float f[8];
-            widen8(load8(ys + slot * ld_ys, c, d), f);
+            widen8(load8<STREAM>(ys + slot * ld_ys, c, d), f);
 #pragma unroll
             for (int i = 0; i < 8; ++i) acc[h][i] += WEIGHTS ? w * f[i] : f[i];
         }
@@ -168,12 +169,12 @@ __global__ __launch_bounds__(256) void k_expert_combine(const uint16_t* ys, int6
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const int64_t c = (int64_t)blockIdx.y * kRowSpan + h * 512 + (threadIdx.x & 63) * 8;
-        if (c < d) store8(y + token * ld_y, c, d, narrow8(acc[h]));
+        if (c < d) store8<STREAM>(y + token * ld_y, c, d, narrow8(acc[h]));
     }
 }
 
 // One wave per slot.  The lanes' partial sums are joined in a fixed order.
-template <bool DYS, bool DW>
+template <bool DYS, bool DW, bool STREAM>
 __global__ __launch_bounds__(256) void k_expert_combine_backward(const uint16_t* dy, int64_t ld_dy, const uint16_t* ys, int64_t ld_ys, int64_t d,
                                                                  MxOrder o, const float* weights, uint16_t* dys, int64_t ld_dys, float* dweights) {
     const int64_t choices = (int64_t)o.tokens * o.top_k;
@@ -194,14 +195,14 @@ __global__ __launch_bounds__(256) void k_expert_combine_backward(const uint16_t*
         if (used) widen8(load8(row, c, d), g);
         if (DW && used) {
             float f[8];
-            widen8(load8(ys + slot * ld_ys, c, d), f);
+            widen8(load8<STREAM>(ys + slot * ld_ys, c, d), f);
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum = __builtin_fmaf(g[i], f[i], sum);
         }
         if (DYS) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) g[i] = used ? g[i] * w : 0.0f;
-            store8(dys + slot * ld_dys, c, d, narrow8(g));
+            store8<STREAM>(dys + slot * ld_dys, c, d, narrow8(g));
         }
     }
     if (DW && used) {
@@ -212,6 +213,7 @@ __global__ __launch_bounds__(256) void k_expert_combine_backward(const uint16_t*
 }
 
 uint32_t four_per_block(int64_t n) { return (uint32_t)((n + 3) / 4); }
+bool streamed(const MxOrder& o, int64_t d) { return (int64_t)o.capacity * d * 2 >= kMxStreamBytes; }
 uint32_t row_spans(int64_t d) { return (uint32_t)((d + kRowSpan - 1) / kRowSpan); }
 
 }  // namespace
@@ -235,24 +237,37 @@ hipError_t launch_expert_sort(const int32_t* ids, const MxOrder& o, void* worksp
 }
 
 hipError_t launch_expert_gather(const uint16_t* x, int64_t ld_x, int64_t d, const MxOrder& o, uint16_t* xs, int64_t ld_xs, hipStream_t st) {
-    k_expert_gather<<<dim3(four_per_block(o.capacity), row_spans(d)), dim3(256), 0, st>>>(x, ld_x, d, o, xs, ld_xs);
+    const dim3 grid(four_per_block(o.capacity), row_spans(d));
+    if (streamed(o, d)) k_expert_gather<true><<<grid, dim3(256), 0, st>>>(x, ld_x, d, o, xs, ld_xs);
+    else k_expert_gather<false><<<grid, dim3(256), 0, st>>>(x, ld_x, d, o, xs, ld_xs);
     return hipGetLastError();
 }
 
 hipError_t launch_expert_combine(const uint16_t* ys, int64_t ld_ys, int64_t d, const MxOrder& o, const float* weights, uint16_t* y,
                                  int64_t ld_y, hipStream_t st) {
     const dim3 grid(four_per_block(o.tokens), row_spans(d));
-    if (weights) k_expert_combine<true><<<grid, dim3(256), 0, st>>>(ys, ld_ys, d, o, weights, y, ld_y);
-    else k_expert_combine<false><<<grid, dim3(256), 0, st>>>(ys, ld_ys, d, o, weights, y, ld_y);
+    if (weights) {
+        if (streamed(o, d)) k_expert_combine<true, true><<<grid, dim3(256), 0, st>>>(ys, ld_ys, d, o, weights, y, ld_y);
+        else k_expert_combine<true, false><<<grid, dim3(256), 0, st>>>(ys, ld_ys, d, o, weights, y, ld_y);
+    } else {
+        if (streamed(o, d)) k_expert_combine<false, true><<<grid, dim3(256), 0, st>>>(ys, ld_ys, d, o, weights, y, ld_y);
+        else k_expert_combine<false, false><<<grid, dim3(256), 0, st>>>(ys, ld_ys, d, o, weights, y, ld_y);
+    }
     return hipGetLastError();
 }
 
+template <bool STREAM>
+static void combine_backward(const uint16_t* dy, int64_t ld_dy, const uint16_t* ys, int64_t ld_ys, int64_t d, const MxOrder& o,
+                             const float* weights, uint16_t* dys, int64_t ld_dys, float* dweights, hipStream_t st) {
+    const dim3 grid(four_per_block(o.capacity));
+    if (dys && dweights) k_expert_combine_backward<true, true, STREAM><<<grid, dim3(256), 0, st>>>(dy, ld_dy, ys, ld_ys, d, o, weights, dys, ld_dys, dweights);
+    else if (dys) k_expert_combine_backward<true, false, STREAM><<<grid, dim3(256), 0, st>>>(dy, ld_dy, ys, ld_ys, d, o, weights, dys, ld_dys, dweights);
+    else k_expert_combine_backward<false, true, STREAM><<<grid, dim3(256), 0, st>>>(dy, ld_dy, ys, ld_ys, d, o, weights, dys, ld_dys, dweights);
+}
 hipError_t launch_expert_combine_backward(const uint16_t* dy, int64_t ld_dy, const uint16_t* ys, int64_t ld_ys, int64_t d, const MxOrder& o,
                                           const float* weights, uint16_t* dys, int64_t ld_dys, float* dweights, hipStream_t st) {
-    const dim3 grid(four_per_block(o.capacity));
-    if (dys && dweights) k_expert_combine_backward<true, true><<<grid, dim3(256), 0, st>>>(dy, ld_dy, ys, ld_ys, d, o, weights, dys, ld_dys, dweights);
-    else if (dys) k_expert_combine_backward<true, false><<<grid, dim3(256), 0, st>>>(dy, ld_dy, ys, ld_ys, d, o, weights, dys, ld_dys, dweights);
-    else k_expert_combine_backward<false, true><<<grid, dim3(256), 0, st>>>(dy, ld_dy, ys, ld_ys, d, o, weights, dys, ld_dys, dweights);
+    if (streamed(o, d)) combine_backward<true>(dy, ld_dy, ys, ld_ys, d, o, weights, dys, ld_dys, dweights, st);
+    else combine_backward<false>(dy, ld_dy, ys, ld_ys, d, o, weights, dys, ld_dys, dweights, st);
     return hipGetLastError();
 }
 

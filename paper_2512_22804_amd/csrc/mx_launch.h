@@ -8,6 +8,11 @@ namespace mor {
 
 constexpr int kMxBlock = 32;            // elements per scale
 
+// Tensors from here on are read and written past the caches (non-temporal): they leave nothing behind that the next call could
+// use.  Measured: 8192 x 4096 from 4 bits to BF16 16.5 us instead of 18.5, 14336 x 4096 27.8 instead of 34.7; 4099 x 5001, which
+// stays in the Infinity Cache, 14.1 instead of 12.8.
+constexpr int64_t kMxStreamBytes = 1 << 26;
+
 // A packed operand on the device: codes and E8M0 bytes, leading dimensions and batch distances in bytes.
 struct MxOperand {
     uint8_t* codes;  int64_t ld;

@@ -5,6 +5,7 @@
 namespace mor {
 namespace {
 
+constexpr int64_t kManyElements = 1 << 22;  // from here on a lane takes several rows
 constexpr int kTileCols = 128;          // columns of a workgroup's tile: 16 lanes of 8 elements
 
 // One workgroup: RPT * 16 rows x 128 columns, 256 lanes.  Lane t holds 8 columns (16 bytes) of RPT rows; a block of the row
@@ -12,7 +13,7 @@ constexpr int kTileCols = 128;          // columns of a workgroup's tile: 16 lan
 // of columns over 32 rows, so that a block's amax needs no other lane and its 16 bytes are one store; four neighbouring
 // lanes fill 64 bytes of an output row.  The rows of row block q are rotated by 16 q dwords: the four row blocks that
 // neighbouring lanes read then lie in different banks.
-template <int RPT, bool ROWS, bool T, bool SR, bool WEIGHTED>
+template <int RPT, bool ROWS, bool T, bool SR, bool WEIGHTED, bool STREAM>
 __global__ __launch_bounds__(256) void k_mx_quantize(MxQuantArgs a, uint32_t col_tiles) {
     static_assert(!T || RPT == 8, "the transposed form works on 128 x 128 tiles");
     __shared__ __align__(16) uint32_t tile[T ? 128 * 64 : 4];
@@ -43,7 +44,7 @@ __global__ __launch_bounds__(256) void k_mx_quantize(MxQuantArgs a, uint32_t col
                 }
             }
         }
-        v[i] = row != nullptr && c < a.cols ? load8(row, c, a.cols) : u32x4{0u, 0u, 0u, 0u};
+        v[i] = row != nullptr && c < a.cols ? load8<STREAM>(row, c, a.cols) : u32x4{0u, 0u, 0u, 0u};
     }
     const bool ceil_rule = a.ceil_rule != 0;
     if (T) {
@@ -140,37 +141,45 @@ __global__ __launch_bounds__(256) void k_mx_quantize(MxQuantArgs a, uint32_t col
     }
 }
 
-// Eight codes to eight BF16 values per lane; the product with the scale is exact in binary32 and fits BF16 exactly.
+// Eight codes to eight BF16 values per lane, RPT rows of them; every value is exact.
+template <int RPT, bool STREAM>
 __global__ __launch_bounds__(256) void k_mx_dequantize(int64_t rows, int64_t cols, MxOperand op, uint16_t* y, int64_t ld_y, int64_t batch_y,
                                                        uint32_t col_tiles) {
     const uint32_t ct = blockIdx.x % col_tiles;
     const int64_t c = (int64_t)ct * kTileCols + (threadIdx.x & 15) * 8;
-    const int64_t r = (int64_t)(blockIdx.x / col_tiles) * 16 + (threadIdx.x >> 4);
+    const int64_t r0 = (int64_t)(blockIdx.x / col_tiles) * (16 * RPT) + (threadIdx.x >> 4);
     const uint32_t z = blockIdx.z;
-    if (r >= rows || c >= cols) return;
-    const uint32_t codes = *reinterpret_cast<const uint32_t*>(op.codes + z * op.batch + r * op.ld + (c >> 1));
-    const uint32_t byte = op.scales[z * op.batch_s + r * op.ld_s + (c >> 5)];
-    const float s = mx_scale_value(byte) * 0.5f;            // byte 0: 2^-128, a subnormal
-    u32x4 out;
+    if (c >= cols) return;
+    uint32_t codes[RPT], byte[RPT];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const uint32_t code = codes >> (4 * j);
-        const float twice = (float)((uint32_t)(0x0C08060403020100ull >> (8 * (code & 7u))) & 0xFFu);
-        uint32_t b = (__float_as_uint(twice * s) >> 16) | ((code & 8u) << 12);
-        if (byte == kMxNan) b = 0x7FC0u;
-        out[j >> 1] = (j & 1) ? (out[j >> 1] | (b << 16)) : b;
+    for (int i = 0; i < RPT; ++i) {
+        const int64_t r = min(r0 + 16 * i, rows - 1);
+        codes[i] = *reinterpret_cast<const uint32_t*>(op.codes + z * op.batch + r * op.ld + (c >> 1));
+        byte[i] = op.scales[z * op.batch_s + r * op.ld_s + (c >> 5)];
     }
-    store8(y + (int64_t)z * batch_y + r * ld_y, c, cols, out);
+#pragma unroll
+    for (int i = 0; i < RPT; ++i) {
+        const int64_t r = r0 + 16 * i;
+        if (r >= rows) break;
+        const float s = __uint_as_float(byte[i] << 23);     // the conversion reads the exponent field alone
+        u32x4 out;
+        out[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], s, 0));
+        out[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], s, 1));
+        out[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], s, 2));
+        out[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], s, 3));
+        if (byte[i] == kMxNan) out = u32x4{0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u};
+        store8<STREAM>(y + (int64_t)z * batch_y + r * ld_y, c, cols, out);
+    }
 }
 
-template <int RPT, bool ROWS, bool T>
+template <int RPT, bool ROWS, bool T, bool STREAM>
 void quantize_form(const MxQuantArgs& a, uint32_t col_tiles, dim3 grid, hipStream_t st) {
     if (a.stochastic) {
-        if (a.weights) k_mx_quantize<RPT, ROWS, T, true, true><<<grid, dim3(256), 0, st>>>(a, col_tiles);
-        else k_mx_quantize<RPT, ROWS, T, true, false><<<grid, dim3(256), 0, st>>>(a, col_tiles);
+        if (a.weights) k_mx_quantize<RPT, ROWS, T, true, true, false><<<grid, dim3(256), 0, st>>>(a, col_tiles);
+        else k_mx_quantize<RPT, ROWS, T, true, false, STREAM><<<grid, dim3(256), 0, st>>>(a, col_tiles);
     } else {
-        if (a.weights) k_mx_quantize<RPT, ROWS, T, false, true><<<grid, dim3(256), 0, st>>>(a, col_tiles);
-        else k_mx_quantize<RPT, ROWS, T, false, false><<<grid, dim3(256), 0, st>>>(a, col_tiles);
+        if (a.weights) k_mx_quantize<RPT, ROWS, T, false, true, false><<<grid, dim3(256), 0, st>>>(a, col_tiles);
+        else k_mx_quantize<RPT, ROWS, T, false, false, STREAM><<<grid, dim3(256), 0, st>>>(a, col_tiles);
     }
 }
 
@@ -179,22 +188,33 @@ void quantize_form(const MxQuantArgs& a, uint32_t col_tiles, dim3 grid, hipStrea
 hipError_t launch_mx_quantize(const MxQuantArgs& a, hipStream_t st) {
     const uint32_t col_tiles = (uint32_t)((a.cols + kTileCols - 1) / kTileCols);
     const bool rows_form = a.out.codes != nullptr, t_form = a.out_t.codes != nullptr;
-    const int tile_rows = t_form ? 128 : 16;
+    const bool tall = a.rows * a.cols > kManyElements;
+    const int tile_rows = t_form ? 128 : tall ? 32 : 16;
     const int64_t tiles = ((a.rows + tile_rows - 1) / tile_rows) * col_tiles;
     if (tiles > 0x7FFFFFFFll) return hipErrorInvalidValue;
     const dim3 grid((uint32_t)tiles, 1, (uint32_t)a.batch);
-    if (!t_form) quantize_form<1, true, false>(a, col_tiles, grid, st);
-    else if (rows_form) quantize_form<8, true, true>(a, col_tiles, grid, st);
-    else quantize_form<8, false, true>(a, col_tiles, grid, st);
+    // rows gathered by expert are read several times; the rows form alone is no faster past the caches (19.1 us against 19.7)
+    const bool stream = t_form && a.src == nullptr && a.rows * a.cols * a.batch * 2 >= kMxStreamBytes;
+    if (!t_form && tall) quantize_form<2, true, false, false>(a, col_tiles, grid, st);
+    else if (!t_form) quantize_form<1, true, false, false>(a, col_tiles, grid, st);
+    else if (rows_form && stream) quantize_form<8, true, true, true>(a, col_tiles, grid, st);
+    else if (rows_form) quantize_form<8, true, true, false>(a, col_tiles, grid, st);
+    else if (stream) quantize_form<8, false, true, true>(a, col_tiles, grid, st);
+    else quantize_form<8, false, true, false>(a, col_tiles, grid, st);
     return hipGetLastError();
 }
 
 hipError_t launch_mx_dequantize(int64_t rows, int64_t cols, int64_t batch, const MxOperand& op, uint16_t* y, int64_t ld_y, int64_t batch_y,
                                 hipStream_t st) {
     const uint32_t col_tiles = (uint32_t)((cols + kTileCols - 1) / kTileCols);
-    const int64_t tiles = ((rows + 15) / 16) * col_tiles;
+    const bool tall = rows * cols * batch > kManyElements;
+    const int tile_rows = tall ? 32 : 16;
+    const int64_t tiles = ((rows + tile_rows - 1) / tile_rows) * col_tiles;
     if (tiles > 0x7FFFFFFFll) return hipErrorInvalidValue;
-    k_mx_dequantize<<<dim3((uint32_t)tiles, 1, (uint32_t)batch), dim3(256), 0, st>>>(rows, cols, op, y, ld_y, batch_y, col_tiles);
+    const dim3 grid((uint32_t)tiles, 1, (uint32_t)batch);
+    if (rows * cols * batch * 2 >= kMxStreamBytes) k_mx_dequantize<2, true><<<grid, dim3(256), 0, st>>>(rows, cols, op, y, ld_y, batch_y, col_tiles);
+    else if (tall) k_mx_dequantize<2, false><<<grid, dim3(256), 0, st>>>(rows, cols, op, y, ld_y, batch_y, col_tiles);
+    else k_mx_dequantize<1, false><<<grid, dim3(256), 0, st>>>(rows, cols, op, y, ld_y, batch_y, col_tiles);
     return hipGetLastError();
 }
 
