@@ -196,6 +196,7 @@ constexpr uint32_t kNowhere = 0x7FFFFFFFu;              // an offset that no ran
 struct RowsBuffer {
     const uint8_t* base;
     int bytes;
+    RowsBuffer() = default;
     __device__ __forceinline__ RowsBuffer(const uint8_t* p, int64_t ld, int64_t row0, int64_t rows, int64_t first, int64_t row_bytes) {
         const uint64_t at = reinterpret_cast<uint64_t>(p + row0 * ld + first);
         // (the halves come back as signed numbers: widened as they are, a low half from 2^31 on would spill into the high one)
@@ -214,9 +215,8 @@ struct RowsBuffer {
 // tracks the builtin's writes into LDS and, not being able to tell the four buffers apart across the loop, waits for all requests
 // before it reads any buffer.  Nothing is loaded into registers here, and the waits stand in multiply_stage.  (M0 is a reserved
 // register: the compiler sets it right before each use of its own, and nothing else in this kernel uses it.)
-__device__ __forceinline__ void load_to_lds(uint32_t lds, u32x4 buffer, uint32_t offset, int group_offset) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
-                 : : "s"(lds), "v"(offset), "s"(buffer), "s"(group_offset) : "memory");
+__device__ __forceinline__ void load_to_lds(uint32_t lds, u32x4 buffer, uint32_t offset) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(lds), "v"(offset), "s"(buffer) : "memory");
 }
 
 template <int BM, int BN>
@@ -242,17 +242,16 @@ template <class S>
 __device__ __forceinline__ void request_codes(uint32_t lds, const Request& q, int stage, int wave, int i) {
     constexpr int kOfA = S::kCodesB / 4096;
     const bool exists = stage <= q.last;
-    if (i < kOfA) load_to_lds(lds + (wave + 4 * i) * 1024, q.a.at(stage * 128, exists), stage == q.last ? q.va_last : q.va, i * q.step_a);
-    else load_to_lds(lds + S::kCodesB + (wave + 4 * (i - kOfA)) * 1024, q.b.at(stage * 128, exists), stage == q.last ? q.vb_last : q.vb,
-                     (i - kOfA) * q.step_b);
+    if (i < kOfA) load_to_lds(lds + (wave + 4 * i) * 1024, q.a.at(stage * 128, exists), (stage == q.last ? q.va_last : q.va) + i * q.step_a);
+    else load_to_lds(lds + S::kCodesB + (wave + 4 * (i - kOfA)) * 1024, q.b.at(stage * 128, exists), (stage == q.last ? q.vb_last : q.vb) + (i - kOfA) * q.step_b);
 }
 // The scales of two stages, 16 bytes of a row.  Wave w loads those of rows 64 w .. + 63 of either operand; where one has fewer, several
 // waves load the same.
 template <class S>
 __device__ __forceinline__ void request_scales(uint32_t lds, const Request& q, int stage, int wave) {
     const bool exists = stage <= q.last;
-    load_to_lds(lds + wave % (S::kScalesB / 1024) * 1024, q.as.at(stage * 8, exists), q.vas, 0);
-    load_to_lds(lds + S::kScalesB + wave % ((S::kScales - S::kScalesB) / 1024) * 1024, q.bs.at(stage * 8, exists), q.vbs, 0);
+    load_to_lds(lds + wave % (S::kScalesB / 1024) * 1024, q.as.at(stage * 8, exists), q.vas);
+    load_to_lds(lds + S::kScalesB + wave % ((S::kScales - S::kScalesB) / 1024) * 1024, q.bs.at(stage * 8, exists), q.vbs);
 }
 
 // A lane's places in a buffer: its pieces of the four steps of a stage, its rows' scales.
@@ -314,8 +313,15 @@ __device__ __forceinline__ void multiply(f32x16& c, u32x4 b, uint32_t sb, u32x4 
         asm("s_nop 1\n\tv_mfma_scale_f32_32x32x64_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[0,0,0] op_sel_hi:[1,1,0] cbsz:4 blgp:4"
             : "+a"(c) : "v"(b), "v"(a), "v"(sb), "v"(sa));
 }
-// The last matrix instruction (eight passes of four cycles) has written its sums.
-__device__ __forceinline__ void settle(f32x16& c) { asm volatile("s_nop 15\n\ts_nop 15" : "+a"(c)); }
+// Before the first other use of the sums: the last matrix instruction (eight passes of four cycles) has written its own.
+template <int FM, int FN>
+__device__ __forceinline__ void settle(f32x16 (&acc)[FM][FN]) {
+    asm volatile("s_nop 15\n\ts_nop 15" : "+a"(acc[FM - 1][FN - 1]));
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) asm volatile("" : "+a"(acc[i][j]));
+}
 
 // Step STEP of a stage: multiplies `cur` and reads `next` from `next_a`, `next_b` (this lane's pieces there), both in slots, one behind
 // each matrix instruction.  From the last step on the requests of stage `ahead` into `to`: a CU takes one of its waves' requests
@@ -361,7 +367,7 @@ __device__ __forceinline__ void multiply_step(f32x16 (&acc)[S::FM][S::FN], const
 // accumulators hold 4 columns of 32 rows.  `kCols` columns at a time; pieces lie permuted by the row against bank conflicts.
 template <bool F32, int FM, int FN, int BYTES>
 __device__ __forceinline__ void store_tile(const MxProductArgs& p, uint8_t* lds, f32x16 (&acc)[FM][FN], int64_t base, int64_t m0, int64_t m_end,
-                                           int64_t n0, int lane) {
+                                           int64_t n0, int lane, bool whole) {
     constexpr int kSize = F32 ? 4 : 2;
     constexpr int kMost = BYTES / (FM * 32) >= 256 ? 256 : 128;                 // bytes of a row at a time
     constexpr int kCols = FN * 32 * kSize > kMost ? kMost / kSize : FN * 32;
@@ -383,8 +389,8 @@ __device__ __forceinline__ void store_tile(const MxProductArgs& p, uint8_t* lds,
                 }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         const int piece = lane % kPieces, first = lane / kPieces;
-        if (p.c_words && n0 + c0 + kCols <= p.n) {
-            // whole rows of 4-byte words: rows from `m_end` on lie outside the buffer
+        if (whole) {
+            // whole rows of 4-byte words: rows from `m_end` on lie outside the buffer; always the same number of stores
             const int64_t rows = min(m_end - m0, (int64_t)FM * 32);
             const uint32_t ld = (uint32_t)p.ldc * kSize;
             const BufRsrc out = make_buf_window(reinterpret_cast<uint8_t*>(p.c) + (base + m0 * p.ldc + n0 + c0) * kSize,
@@ -414,44 +420,111 @@ __device__ __forceinline__ void store_tile(const MxProductArgs& p, uint8_t* lds,
     }
 }
 
-template <int MODE, bool F32, int BM, int BN, int GROUPS>
-__global__ __launch_bounds__(256, GROUPS) void k_mx_tile(MxProductArgs p, uint32_t m_tiles, uint32_t n_tiles) {
-    typedef TileShape<BM, BN> S;
-    constexpr int FM = S::FM, FN = S::FN;
-    __shared__ __align__(1024) uint8_t lds[S::kLds];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    // Workgroups go to the eight XCDs in turn; each XCD takes a run of tiles, in patches of 8 tile rows, so that the tiles at work
-    // together share their operands in its L2.
-    uint32_t id = blockIdx.x;
-    {
-        const uint32_t total = gridDim.x, each = total / 8, more = total % 8, x = id % 8;
-        id = x * each + min(x, more) + id / 8;
-    }
-    uint32_t z = 0;
-    if (MODE != kMxRows) { z = id / (m_tiles * n_tiles); id -= z * (m_tiles * n_tiles); }
-    const uint32_t patch = id / (8 * n_tiles), in_patch = id - patch * (8 * n_tiles);
-    const uint32_t tall = min(8u, m_tiles - patch * 8);
-    const uint32_t m_tile = patch * 8 + in_patch % tall, n_tile = in_patch / tall;
+// A tile and what its requests need.
+template <class S>
+struct TileWork {
     Tile t;
-    if (!find_tile<MODE>(p, m_tile, z, BM, &t)) return;
-    const int64_t n0 = (int64_t)n_tile * BN;
-    const int blocks = __builtin_amdgcn_readfirstlane(t.k_end - t.k0);
-    const int stages = (blocks + 7) / 8;
+    int64_t n0;
+    int blocks, stages;
+    Request q;
+};
 
+// Values that are the same in every lane, which the compiler cannot see where they come out of a search by all lanes.
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ int64_t uniform(int64_t v) {
+    const uint32_t low = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)v), high = (uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32));
+    return (int64_t)(((uint64_t)high << 32) | low);
+}
+__device__ __forceinline__ void make_uniform(RowsBuffer* b) {
+    b->base = reinterpret_cast<const uint8_t*>(uniform((int64_t)reinterpret_cast<uintptr_t>(b->base)));
+    b->bytes = uniform(b->bytes);
+}
+template <class S>
+__device__ __forceinline__ void make_uniform(TileWork<S>* w) {
+    make_uniform(&w->q.a);
+    make_uniform(&w->q.as);
+    make_uniform(&w->q.b);
+    make_uniform(&w->q.bs);
+    w->q.last = uniform(w->q.last);
+    w->blocks = uniform(w->blocks);
+    w->stages = uniform(w->stages);
+    w->t.m0 = uniform(w->t.m0);
+    w->t.m_end = uniform(w->t.m_end);
+    w->t.expert = uniform(w->t.expert);
+    w->n0 = uniform(w->n0);
+}
+
+// The tiles of a workgroup, one after the other.  The XCDs take the workgroups in turn; each gets a run of tiles, in patches of 8
+// tile rows, so that the tiles at work together share their operands in its L2.
+struct Walk {
+    uint32_t left;                      // tiles of this XCD's run from the present one on
+    uint32_t z, patch, in_patch;        // expert or part, patch, tile in it
+    uint32_t n_tiles, m_tiles, stride;
+    __device__ __forceinline__ Walk(uint32_t total, uint32_t mt, uint32_t nt, bool many) {
+        const uint32_t x = blockIdx.x % 8, run = total / 8 + (x < total % 8 ? 1u : 0u);
+        uint32_t id = x * (total / 8) + min(x, total % 8) + blockIdx.x / 8;
+        left = run > blockIdx.x / 8 ? run - blockIdx.x / 8 : 0u;
+        n_tiles = nt; m_tiles = mt;
+        stride = (gridDim.x - x + 7) / 8;       // workgroups of this XCD
+        z = many ? id / (mt * nt) : 0u;
+        id -= z * (mt * nt);
+        patch = id / (8 * nt);
+        in_patch = id - patch * (8 * nt);
+    }
+    __device__ __forceinline__ void next(bool many) {
+        left = left > stride ? left - stride : 0u;
+        in_patch += stride;
+        for (;;) {                      // a few times at most: patches hold 8 n_tiles tiles, the last one of an expert fewer
+            const uint32_t size = min(8u, m_tiles - patch * 8) * n_tiles;
+            if (in_patch < size || !left) break;
+            in_patch -= size;
+            if (++patch * 8 >= m_tiles && many) { patch = 0; ++z; }
+        }
+    }
+};
+
+template <int MODE, int BM, int BN, class S>
+__device__ __forceinline__ bool find_work(const MxProductArgs& p, const Walk& walk, int lane, int wave, TileWork<S>* w) {
+    const uint32_t tall = min(8u, walk.m_tiles - walk.patch * 8), z = walk.z;
+    uint32_t in_patch = walk.in_patch;
+    const uint32_t n_tile = tall == 8 ? in_patch / 8 : in_patch / tall, m_tile = walk.patch * 8 + (in_patch - n_tile * tall);
+    Tile& t = w->t;
+    if (!find_tile<MODE>(p, m_tile, z, BM, &t)) return false;
+    w->n0 = (int64_t)n_tile * BN;
+    w->blocks = __builtin_amdgcn_readfirstlane(t.k_end - t.k0);
+    w->stages = max((w->blocks + 7) / 8, 1);             // (no depth at all: one stage of zeros)
     const int64_t row_bytes = (int64_t)p.blocks * 16, row_scales = ((int64_t)p.blocks + 3) & ~3ll;
-    const int64_t rows_a = min((int64_t)BM, t.m_end - t.m0), rows_b = min((int64_t)BN, p.n - n0);
+    const int64_t rows_a = min((int64_t)BM, t.m_end - t.m0), rows_b = min((int64_t)BN, p.n - w->n0);
     const int64_t of_b = MODE == kMxRows ? t.expert * p.batch_b : 0, of_bs = MODE == kMxRows ? t.expert * p.batch_bs : 0;
     const int piece = (lane & 7) ^ ((lane >> 4) + 4 * (wave & 1));      // of row lane / 8 of a group of 8
-    const bool piece_in = (stages - 1) * 8 + piece < blocks;
-    Request q{RowsBuffer(p.a, p.lda, t.m0, rows_a, (int64_t)t.k0 * 16, row_bytes), RowsBuffer(p.as, p.lda_s, t.m0, rows_a, t.k0, row_scales),
-              RowsBuffer(p.b + of_b, p.ldb, n0, rows_b, (int64_t)t.k0 * 16, row_bytes),
-              RowsBuffer(p.bs + of_bs, p.ldb_s, n0, rows_b, t.k0, row_scales),
-              (uint32_t)(wave * 8 + (lane >> 3)) * (uint32_t)p.lda + piece * 16, (uint32_t)(wave * 8 + (lane >> 3)) * (uint32_t)p.ldb + piece * 16,
-              (uint32_t)(wave % (BM / 64) * 64 + lane) * (uint32_t)p.lda_s, (uint32_t)(wave % (BN / 64) * 64 + lane) * (uint32_t)p.ldb_s, 0u, 0u,
-              (int)p.lda * 32, (int)p.ldb * 32, stages - 1};
+    const bool piece_in = (w->stages - 1) * 8 + piece < w->blocks;
+    Request& q = w->q;
+    q.a = RowsBuffer(p.a, p.lda, t.m0, rows_a, (int64_t)t.k0 * 16, row_bytes);
+    q.as = RowsBuffer(p.as, p.lda_s, t.m0, rows_a, t.k0, row_scales);
+    q.b = RowsBuffer(p.b + of_b, p.ldb, w->n0, rows_b, (int64_t)t.k0 * 16, row_bytes);
+    q.bs = RowsBuffer(p.bs + of_bs, p.ldb_s, w->n0, rows_b, t.k0, row_scales);
+    q.va = (uint32_t)(wave * 8 + (lane >> 3)) * (uint32_t)p.lda + piece * 16;
+    q.vb = (uint32_t)(wave * 8 + (lane >> 3)) * (uint32_t)p.ldb + piece * 16;
+    q.vas = (uint32_t)(wave % (BM / 64) * 64 + lane) * (uint32_t)p.lda_s;
+    q.vbs = (uint32_t)(wave % (BN / 64) * 64 + lane) * (uint32_t)p.ldb_s;
     q.va_last = piece_in ? q.va : kNowhere;
     q.vb_last = piece_in ? q.vb : kNowhere;
+    q.step_a = (int)p.lda * 32;
+    q.step_b = (int)p.ldb * 32;
+    q.last = w->stages - 1;
+    return true;
+}
 
+// Workgroups stay and take tile after tile: the next tile's first stage is on its way while the sums go out by way of the second
+// buffer.
+template <int MODE, bool F32, int BM, int BN, int GROUPS>
+__global__ __launch_bounds__(256, GROUPS) void k_mx_tile(MxProductArgs p, uint32_t total, uint32_t m_tiles, uint32_t n_tiles) {
+    typedef TileShape<BM, BN> S;
+    constexpr int FM = S::FM, FN = S::FN;
+    constexpr int kStores = FM * FN * 32 * 32 * (F32 ? 4 : 2) / 1024;           // of a wave's tile in whole rows
+    constexpr int kAfterStores = kStores + S::kFirstRequests < 63 ? kStores + S::kFirstRequests : 63;
+    __shared__ __align__(1024) uint8_t lds[S::kLds];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int row = lane & 31;
     const uint32_t half = lane >> 5;
     const int wm = (wave >> 1) * (BM / 2), wn = (wave & 1) * (BN / 2);
@@ -464,61 +537,78 @@ __global__ __launch_bounds__(256, GROUPS) void k_mx_tile(MxProductArgs p, uint32
     }
     at.sa = (wm + row) * 16;
     at.sb = S::kScalesB + (wn + row) * 16;
+    const uint32_t lds_at = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) uint8_t*)lds);
+    const uint8_t* lds_scales = lds + S::kScalesAt;
 
-    f32x16 acc[FM][FN];
+    TileWork<S> w;
+    Walk walk(total, m_tiles, n_tiles, MODE != kMxRows);
+    while (walk.left && !find_work<MODE, BM, BN>(p, walk, lane, wave, &w)) walk.next(MODE != kMxRows);
+    if (!walk.left) return;
+    make_uniform(&w);
+    request_scales<S>(lds_at + S::kScalesAt, w.q, 0, wave);
 #pragma unroll
-    for (int i = 0; i < FM; ++i)
+    for (int i = 0; i < S::kRequests; ++i) request_codes<S>(lds_at, w.q, 0, wave, i);
+    bool stored = false;                                // whole rows were, kStores of them behind the first stage's requests
+    for (;;) {
 #pragma unroll
-        for (int j = 0; j < FN; ++j) acc[i][j] = f32x16{};
-    if (stages > 0) {
+        for (int i = 0; i < S::kFirstRequests; ++i) request_codes<S>(lds_at + S::kCodes, w.q, 1, wave, i);
+        f32x16 acc[FM][FN];
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j) acc[i][j] = f32x16{};
         Fragments<FM, FN> f0, f1;
         Scales<FM, FN> sc;
-        const uint32_t lds_at = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) uint8_t*)lds);
-        const uint8_t* lds_scales = lds + S::kScalesAt;
-        request_scales<S>(lds_at + S::kScalesAt, q, 0, wave);
-#pragma unroll
-        for (int i = 0; i < S::kRequests; ++i) request_codes<S>(lds_at, q, 0, wave, i);
-#pragma unroll
-        for (int i = 0; i < S::kFirstRequests; ++i) request_codes<S>(lds_at + S::kCodes, q, 1, wave, i);
-        __builtin_amdgcn_s_waitcnt(0x0F70 | S::kFirstRequests);
+        // the first stage is here
+        if (stored) __builtin_amdgcn_s_waitcnt(0x0F70 | (kAfterStores & 15) | (kAfterStores >> 4 << 14));
+        else __builtin_amdgcn_s_waitcnt(0x0F70 | S::kFirstRequests);
         __syncthreads();
         read_fragments(f0, lds, at, 0);
         {
-            const ScaleMask mask(blocks, half);
+            const ScaleMask mask(w.blocks, half);
 #pragma unroll
             for (int i = 0; i < FM; ++i) sc.a[i] = mask(*reinterpret_cast<const u32x2*>(lds_scales + at.sa + i * 512));
 #pragma unroll
             for (int j = 0; j < FN; ++j) sc.b[j] = mask(*reinterpret_cast<const u32x2*>(lds_scales + at.sb + j * 512));
         }
         uint32_t cur = 0u;                              // buffer of the stage
-        for (int s = 0; s < stages; ++s) {
+        for (int s = 0; s < w.stages; ++s) {
             const uint8_t *here = lds + cur, *there = lds + (S::kCodes - cur);
             // the next stage's scales: pairs of stages take turns in two buffers
             const uint8_t* sc_next = lds_scales + ((s + 1) >> 1 & 1) * S::kScales + ((s + 1) & 1) * 8;
             const uint32_t to_here = lds_at + cur, to_there = lds_at + (S::kCodes - cur);
-            const ScaleMask mask(blocks - (s + 1) * 8, half);
+            const ScaleMask mask(w.blocks - (s + 1) * 8, half);
             Scales<FM, FN> fresh;
-            multiply_step<0, S>(acc, f0, f1, sc, fresh, here + at.a[1], here + at.b[1], sc_next + at.sa, sc_next + at.sb, to_there, q, s + 1, wave, mask);
-            multiply_step<1, S>(acc, f1, f0, sc, fresh, here + at.a[2], here + at.b[2], sc_next + at.sa, sc_next + at.sb, to_there, q, s + 1, wave, mask);
-            multiply_step<2, S>(acc, f0, f1, sc, fresh, here + at.a[3], here + at.b[3], sc_next + at.sa, sc_next + at.sb, to_there, q, s + 1, wave, mask);
+            multiply_step<0, S>(acc, f0, f1, sc, fresh, here + at.a[1], here + at.b[1], sc_next + at.sa, sc_next + at.sb, to_there, w.q, s + 1, wave, mask);
+            multiply_step<1, S>(acc, f1, f0, sc, fresh, here + at.a[2], here + at.b[2], sc_next + at.sa, sc_next + at.sb, to_there, w.q, s + 1, wave, mask);
+            multiply_step<2, S>(acc, f0, f1, sc, fresh, here + at.a[3], here + at.b[3], sc_next + at.sa, sc_next + at.sb, to_there, w.q, s + 1, wave, mask);
             __builtin_amdgcn_s_waitcnt(0x0070);         // this wave's reads of the stage are complete, its requests of the next one too
             __syncthreads();
-            if ((s & 1) == 0) request_scales<S>(lds_at + S::kScalesAt + ((s >> 1) + 1 & 1) * S::kScales, q, s + 2, wave);
-            multiply_step<3, S>(acc, f1, f0, sc, fresh, there + at.a[0], there + at.b[0], sc_next + at.sa, sc_next + at.sb, to_here, q, s + 2, wave, mask);
+            if ((s & 1) == 0) request_scales<S>(lds_at + S::kScalesAt + ((s >> 1) + 1 & 1) * S::kScales, w.q, s + 2, wave);
+            multiply_step<3, S>(acc, f1, f0, sc, fresh, there + at.a[0], there + at.b[0], sc_next + at.sa, sc_next + at.sb, to_here, w.q, s + 2, wave, mask);
             sc = fresh;
             cur = S::kCodes - cur;
         }
-        __builtin_amdgcn_s_waitcnt(0x0F70);             // the empty requests too, before the buffers are written
+        // this tile's place in C, then the next tile
+        const int64_t base = MODE != kMxRows ? w.t.expert * p.batch_c : 0, m0 = w.t.m0 + wm, m_end = w.t.m_end, n0 = w.n0 + wn;
+        do walk.next(MODE != kMxRows);
+        while (walk.left && !find_work<MODE, BM, BN>(p, walk, lane, wave, &w));
+        __builtin_amdgcn_s_waitcnt(0x0070);             // the empty requests too, before the buffers are written; the last reads
+        __syncthreads();
+        if (walk.left) {
+            make_uniform(&w);
+            request_scales<S>(lds_at + S::kScalesAt, w.q, 0, wave);
+#pragma unroll
+            for (int i = 0; i < S::kRequests; ++i) request_codes<S>(lds_at, w.q, 0, wave, i);
+        }
+        settle(acc);
+        stored = p.c_words && n0 + FN * 32 <= p.n;
+        int own_lane = lane;                            // (as if new for every tile: its addresses are not kept in registers all along)
+        asm volatile("" : "+v"(own_lane));
+        store_tile<F32, FM, FN, S::kCodes / 4>(p, lds + S::kCodes + wave * (S::kCodes / 4), acc, base, m0, m_end, n0, own_lane, stored);
+        if (!walk.left) break;
+        __syncthreads();                                // every wave has read what it put into the second buffer
     }
-#pragma unroll
-    for (int i = 0; i < FM; ++i)
-#pragma unroll
-        for (int j = 0; j < FN; ++j) settle(acc[i][j]);
-    __syncthreads();
-    constexpr int kShare = S::kLds / 4 & ~1023;
-    uint8_t* mine = lds + wave * kShare;
-    const int64_t base = MODE != kMxRows ? t.expert * p.batch_c : 0;
-    store_tile<F32, FM, FN, kShare>(p, mine, acc, base, t.m0 + wm, t.m_end, n0 + wn, lane);
 }
 
 // ---- few rows ---------------------------------------------------------------------------------------------------------
@@ -649,6 +739,7 @@ size_t mx_product_workspace(int64_t m, int64_t n, int64_t blocks) {
     return splits == 1 ? 0 : (size_t)splits * m * part_ld(n) * 4;
 }
 
+constexpr int64_t kCus = 256;            // of an MI355X
 template <bool F32, int BM, int BN, int GROUPS>
 static hipError_t launch_tiles(int mode, const MxProductArgs& p, hipStream_t st) {
     const int64_t n_tiles = (p.n + BN - 1) / BN;
@@ -656,10 +747,11 @@ static hipError_t launch_tiles(int mode, const MxProductArgs& p, hipStream_t st)
     if (mode == kMxRows) m_tiles = p.m / BM + std::min<int64_t>(p.n_experts, p.m);
     const int64_t total = n_tiles * m_tiles * (mode == kMxDepth ? p.n_experts : p.splits);
     if (total > 0x7FFFFFFFll) return hipErrorInvalidValue;
-    const dim3 grid((uint32_t)total);
-    if (mode == kMxDense) k_mx_tile<kMxDense, F32, BM, BN, GROUPS><<<grid, dim3(256), 0, st>>>(p, (uint32_t)m_tiles, (uint32_t)n_tiles);
-    else if (mode == kMxRows) k_mx_tile<kMxRows, F32, BM, BN, GROUPS><<<grid, dim3(256), 0, st>>>(p, (uint32_t)m_tiles, (uint32_t)n_tiles);
-    else k_mx_tile<kMxDepth, F32, BM, BN, GROUPS><<<grid, dim3(256), 0, st>>>(p, (uint32_t)m_tiles, (uint32_t)n_tiles);
+    const dim3 grid((uint32_t)std::min<int64_t>(total, kCus * GROUPS));
+    const uint32_t tiles = (uint32_t)total, mt = (uint32_t)m_tiles, nt = (uint32_t)n_tiles;
+    if (mode == kMxDense) k_mx_tile<kMxDense, F32, BM, BN, GROUPS><<<grid, dim3(256), 0, st>>>(p, tiles, mt, nt);
+    else if (mode == kMxRows) k_mx_tile<kMxRows, F32, BM, BN, GROUPS><<<grid, dim3(256), 0, st>>>(p, tiles, mt, nt);
+    else k_mx_tile<kMxDepth, F32, BM, BN, GROUPS><<<grid, dim3(256), 0, st>>>(p, tiles, mt, nt);
     return hipGetLastError();
 }
 
