@@ -9,7 +9,8 @@ namespace {
 
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
 constexpr int kMaxExperts = 1024;       // one lane each
-constexpr int kSortChunk = 4096;        // choices of a workgroup
+constexpr int64_t kSortLone = 4096;     // choices that one workgroup sorts alone: 5.9 us for 1332, two launches take 8 and more
+constexpr int64_t kSortChunks = 256;    // workgroups at most, each of which sums up the counts of all
 
 __device__ __forceinline__ uint32_t expert_of(const int32_t* ids, int64_t i, int64_t n, uint32_t experts) {
     const uint32_t e = i < n ? (uint32_t)ids[i] : experts;
@@ -17,13 +18,12 @@ __device__ __forceinline__ uint32_t expert_of(const int32_t* ids, int64_t i, int
 }
 
 // Choices of each expert in each chunk; integer sums, so their order does not matter.
-__global__ __launch_bounds__(kSortThreads) void k_expert_count(const int32_t* ids, int64_t choices, uint32_t experts, uint32_t* counts) {
+__global__ __launch_bounds__(kSortThreads) void k_expert_count(const int32_t* ids, int64_t choices, uint32_t experts, uint32_t* counts, int rounds) {
     __shared__ uint32_t hist[kMaxExperts + 1];
     for (uint32_t e = threadIdx.x; e <= experts; e += kSortThreads) hist[e] = 0u;
     __syncthreads();
-    const int64_t i0 = (int64_t)blockIdx.x * kSortChunk;
-#pragma unroll
-    for (int j = 0; j < kSortChunk / kSortThreads; ++j) {
+    const int64_t i0 = (int64_t)blockIdx.x * rounds * kSortThreads;
+    for (int j = 0; j < rounds; ++j) {
         const uint32_t e = expert_of(ids, i0 + j * kSortThreads + threadIdx.x, choices, experts);
         if (e < experts) atomicAdd(&hist[e], 1u);
     }
@@ -51,7 +51,7 @@ __device__ __forceinline__ uint32_t scan_before(uint32_t v, uint32_t* wave_sums)
 // Lane e holds expert e's sums.  Within 64 choices the lanes of one expert find each other by ballots over the bits of its number,
 // so a choice's rank needs no atomic and the order is the choices' own.
 template <bool LONE>
-__global__ __launch_bounds__(kSortThreads) void k_expert_place(const int32_t* ids, int64_t choices, const uint32_t* counts, MxOrder o) {
+__global__ __launch_bounds__(kSortThreads) void k_expert_place(const int32_t* ids, int64_t choices, const uint32_t* counts, MxOrder o, int rounds) {
     __shared__ uint32_t next[kMaxExperts + 1];              // slot of the expert's next choice
     __shared__ uint32_t wave_sums[kSortWaves];
     __shared__ uint8_t in_wave[kSortWaves][kMaxExperts];    // choices of the expert among a wave's 64
@@ -92,8 +92,8 @@ __global__ __launch_bounds__(kSortThreads) void k_expert_place(const int32_t* id
     __syncthreads();
     for (int64_t s = (int64_t)end + blockIdx.x * kSortThreads + threadIdx.x; s < o.capacity; s += (int64_t)chunks * kSortThreads) o.src[s] = -1;
 
-    const int64_t i0 = (int64_t)blockIdx.x * kSortChunk;
-    for (int j = 0; j < kSortChunk / kSortThreads; ++j) {
+    const int64_t i0 = (int64_t)blockIdx.x * rounds * kSortThreads;
+    for (int j = 0; j < rounds; ++j) {
         const int64_t i = i0 + j * kSortThreads + threadIdx.x;
         if (i0 + j * kSortThreads >= choices) break;
         for (uint32_t q = threadIdx.x; q < kSortWaves * kMaxExperts / 4; q += kSortThreads) reinterpret_cast<uint32_t*>(in_wave)[q] = 0u;
@@ -151,19 +151,35 @@ __global__ __launch_bounds__(256) void k_expert_combine(const uint16_t* ys, int6
     const int64_t token = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (token >= o.tokens) return;
     float acc[2][8] = {};
-    for (int j = 0; j < o.top_k; ++j) {
-        const int64_t choice = token * o.top_k + j;
-        const uint32_t slot = (uint32_t)o.slot_of[choice];
-        if (slot >= (uint32_t)o.capacity) continue;
-        const float w = WEIGHTS ? weights[choice] : 1.0f;
+    // the rows of up to four choices are on their way at once; they are added in order
+    constexpr int kAtOnce = 4;
+    for (int j0 = 0; j0 < o.top_k; j0 += kAtOnce) {
+        uint32_t slot[kAtOnce];
+        float w[kAtOnce];
+        u32x4 rows[kAtOnce][2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int64_t c = (int64_t)blockIdx.y * kRowSpan + h * 512 + (threadIdx.x & 63) * 8;
-            if (c >= d) continue;
-            float f[8];
-            widen8(load8<STREAM>(ys + slot * ld_ys, c, d), f);
+        for (int j = 0; j < kAtOnce; ++j) {
+            const int64_t choice = token * o.top_k + j0 + j;
+            slot[j] = j0 + j < o.top_k ? (uint32_t)o.slot_of[choice] : ~0u;
+            w[j] = WEIGHTS && j0 + j < o.top_k ? weights[choice] : 1.0f;
+        }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) acc[h][i] += WEIGHTS ? w * f[i] : f[i];
+        for (int j = 0; j < kAtOnce; ++j)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int64_t c = (int64_t)blockIdx.y * kRowSpan + h * 512 + (threadIdx.x & 63) * 8;
+                rows[j][h] = slot[j] < (uint32_t)o.capacity && c < d ? load8<STREAM>(ys + slot[j] * ld_ys, c, d) : u32x4{0u, 0u, 0u, 0u};
+            }
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) {
+            if (slot[j] >= (uint32_t)o.capacity) continue;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float f[8];
+                widen8(rows[j][h], f);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) acc[h][i] += WEIGHTS ? w[j] * f[i] : f[i];
+            }
         }
     }
 #pragma unroll
@@ -218,20 +234,30 @@ uint32_t row_spans(int64_t d) { return (uint32_t)((d + kRowSpan - 1) / kRowSpan)
 
 }  // namespace
 
+// Rounds of 1024 choices per workgroup, and workgroups.
+static int sort_rounds(int64_t choices) {
+    if (choices <= kSortLone) return (int)std::max<int64_t>((choices + kSortThreads - 1) / kSortThreads, 1);
+    return (int)((choices + kSortChunks * kSortThreads - 1) / (kSortChunks * kSortThreads));
+}
+static int64_t sort_chunks(int64_t choices) {
+    const int64_t each = (int64_t)sort_rounds(choices) * kSortThreads;
+    return std::max<int64_t>((choices + each - 1) / each, 1);
+}
+
 size_t mx_sort_workspace(int64_t choices, int64_t n_experts) {
-    const int64_t chunks = (choices + kSortChunk - 1) / kSortChunk;
+    const int64_t chunks = sort_chunks(choices);
     return chunks <= 1 ? 0 : (size_t)(chunks * n_experts * 4 + 15) / 16 * 16;
 }
 
 hipError_t launch_expert_sort(const int32_t* ids, const MxOrder& o, void* workspace, hipStream_t st) {
-    const int64_t choices = (int64_t)o.tokens * o.top_k;
-    const int64_t chunks = (choices + kSortChunk - 1) / kSortChunk;
+    const int64_t choices = (int64_t)o.tokens * o.top_k, chunks = sort_chunks(choices);
+    const int rounds = sort_rounds(choices);
     if (chunks <= 1) {
-        k_expert_place<true><<<dim3(1), dim3(kSortThreads), 0, st>>>(ids, choices, nullptr, o);
+        k_expert_place<true><<<dim3(1), dim3(kSortThreads), 0, st>>>(ids, choices, nullptr, o, rounds);
     } else {
         uint32_t* counts = static_cast<uint32_t*>(workspace);
-        k_expert_count<<<dim3((uint32_t)chunks), dim3(kSortThreads), 0, st>>>(ids, choices, (uint32_t)o.n_experts, counts);
-        k_expert_place<false><<<dim3((uint32_t)chunks), dim3(kSortThreads), 0, st>>>(ids, choices, counts, o);
+        k_expert_count<<<dim3((uint32_t)chunks), dim3(kSortThreads), 0, st>>>(ids, choices, (uint32_t)o.n_experts, counts, rounds);
+        k_expert_place<false><<<dim3((uint32_t)chunks), dim3(kSortThreads), 0, st>>>(ids, choices, counts, o, rounds);
     }
     return hipGetLastError();
 }

@@ -17,7 +17,7 @@ template <int RPT, bool ROWS, bool T, bool SR, bool WEIGHTED, bool STREAM>
 __global__ __launch_bounds__(256) void k_mx_quantize(MxQuantArgs a, uint32_t col_tiles) {
     static_assert(!T || RPT == 8, "the transposed form works on 128 x 128 tiles");
     __shared__ __align__(16) uint32_t tile[T ? 128 * 64 : 4];
-    __shared__ float row_weight[WEIGHTED ? RPT * 16 : 1];
+    __shared__ __align__(16) float row_weight[WEIGHTED ? RPT * 16 : 1];
     const int t = threadIdx.x;
     const uint32_t ct = blockIdx.x % col_tiles;
     const int64_t rt = blockIdx.x / col_tiles;
@@ -97,34 +97,41 @@ __global__ __launch_bounds__(256) void k_mx_quantize(MxQuantArgs a, uint32_t col
         const int q = t & 3, pair = t >> 2;
         const int64_t col = c0 + 2 * pair, row0 = r0 + 32 * q;
         uint32_t d[32];
-        uint32_t m = 0u;
-        float wa = 0.0f;
-        uint32_t amax0 = 0u, amax1 = 0u;
 #pragma unroll
-        for (int j = 0; j < 32; ++j) {
-            d[j] = tile[(32 * q + j) * 64 + ((pair + 16 * q) & 63)];
-            if (WEIGHTED) {
-                wa = row_weight[32 * q + j];
-                amax0 = max(amax0, __float_as_uint(__uint_as_float(d[j] << 16) * wa) & 0x7FFFFFFFu);
-                amax1 = max(amax1, __float_as_uint(__uint_as_float(d[j] & 0xFFFF0000u) * wa) & 0x7FFFFFFFu);
-            } else m = pk_max_u16(m, d[j] & 0x7FFF7FFFu);
+        for (int j = 0; j < 32; ++j) d[j] = tile[(32 * q + j) * 64 + ((pair + 16 * q) & 63)];
+        uint32_t m = 0u;
+        float w32[WEIGHTED ? 32 : 1];
+        if (WEIGHTED) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) w32[j] = row_weight[32 * q + j];
+        } else {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) m = pk_max_u16(m, d[j] & 0x7FFF7FFFu);
         }
-        if (!WEIGHTED) { amax0 = m << 16; amax1 = m & 0xFFFF0000u; }
 #pragma unroll
         for (int side = 0; side < 2; ++side) {
-            const uint32_t byte = mx_scale_byte(side ? amax1 : amax0, ceil_rule);
+            float f[32];
+            uint32_t amax = side ? m & 0xFFFF0000u : m << 16;
+            if (SR || WEIGHTED) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j) {
+                    f[j] = __uint_as_float(side ? (d[j] & 0xFFFF0000u) : (d[j] << 16));
+                    if (WEIGHTED) {
+                        f[j] *= w32[j];
+                        amax = max(amax, __float_as_uint(f[j]) & 0x7FFFFFFFu);
+                    }
+                }
+            }
+            const uint32_t byte = mx_scale_byte(amax, ceil_rule);
             u32x4 codes;
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 if (SR || WEIGHTED) {
-                    float f[8];
+                    float f8[8];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        f[j] = __uint_as_float(side ? (d[8 * g + j] & 0xFFFF0000u) : (d[8 * g + j] << 16));
-                        if (WEIGHTED) f[j] *= row_weight[32 * q + 8 * g + j];
-                    }
-                    if (SR) codes[g] = mx_codes8_stochastic(f, byte, philox((uint32_t)(row0 >> 3) + g, (uint32_t)(col + side), z, 1u, k0, k1));
-                    else codes[g] = mx_codes8_nearest(f, byte);
+                    for (int j = 0; j < 8; ++j) f8[j] = f[8 * g + j];
+                    if (SR) codes[g] = mx_codes8_stochastic(f8, byte, philox((uint32_t)(row0 >> 3) + g, (uint32_t)(col + side), z, 1u, k0, k1));
+                    else codes[g] = mx_codes8_nearest(f8, byte);
                 } else {
                     u32x4 p;
 #pragma unroll
