@@ -94,6 +94,7 @@ mor_status mor_mx_quantize(const mor_mx_params* p, const uint16_t* x, const mor_
     a.x = x; a.rows = rows; a.cols = p->cols; a.ld = p->ld; a.batch_x = batched ? p->batch_x : 0; a.batch = (int32_t)p->batch;
     if (order) {
         a.src = order->src;
+        a.slot_of = order->slot_of;
         a.choices = (uint32_t)order->tokens * (uint32_t)order->top_k;
         a.top_k = (uint32_t)order->top_k;
         a.weights = weights;

@@ -33,6 +33,7 @@ struct MxQuantArgs {
     int64_t  rows, cols, ld, batch_x;   // rows of the output (slots when `src` is set)
     int32_t  batch;
     const int32_t* src;                 // choice of each row, or nullptr: row r of x is row r
+    const int32_t* slot_of;             // slot of each choice (with `src`)
     uint32_t choices, top_k;
     const float* weights;               // factor of each choice, or nullptr
     int      ceil_rule;

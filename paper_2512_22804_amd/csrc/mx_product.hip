@@ -365,7 +365,7 @@ __device__ __forceinline__ void multiply_step(f32x16 (&acc)[S::FM][S::FN], const
 
 // A wave's sums to C by way of its LDS buffer, so that every row is written in pieces of 16 neighbouring bytes per lane: the
 // accumulators hold 4 columns of 32 rows.  `kCols` columns at a time; pieces lie permuted by the row against bank conflicts.
-template <bool F32, int FM, int FN, int BYTES>
+template <bool F32, int FM, int FN, int BYTES, int AUX>
 __device__ __forceinline__ void store_tile(const MxProductArgs& p, uint8_t* lds, f32x16 (&acc)[FM][FN], int64_t base, int64_t m0, int64_t m_end,
                                            int64_t n0, int lane, bool whole) {
     constexpr int kSize = F32 ? 4 : 2;
@@ -399,7 +399,7 @@ __device__ __forceinline__ void store_tile(const MxProductArgs& p, uint8_t* lds,
 #pragma unroll
             for (int r = 0; r < FM * 32; r += kLanes) {
                 const int row_r = first + r;            // its swizzle repeats: kLanes divides kPieces or the other way round
-                buf_store16<0>(out, at, *reinterpret_cast<const u32x4*>(lds + row_r * kRow + (piece ^ (row_r & (kPieces - 1))) * 16));
+                buf_store16<AUX>(out, at, *reinterpret_cast<const u32x4*>(lds + row_r * kRow + (piece ^ (row_r & (kPieces - 1))) * 16));
                 at += kLanes * ld;
             }
         } else {
@@ -605,7 +605,7 @@ __global__ __launch_bounds__(256, GROUPS) void k_mx_tile(MxProductArgs p, uint32
         stored = p.c_words && n0 + FN * 32 <= p.n;
         int own_lane = lane;                            // (as if new for every tile: its addresses are not kept in registers all along)
         asm volatile("" : "+v"(own_lane));
-        store_tile<F32, FM, FN, S::kCodes / 4>(p, lds + S::kCodes + wave * (S::kCodes / 4), acc, base, m0, m_end, n0, own_lane, stored);
+        store_tile<F32, FM, FN, S::kCodes / 4, MODE == kMxDepth ? kBufStoreAux : 0>(p, lds + S::kCodes + wave * (S::kCodes / 4), acc, base, m0, m_end, n0, own_lane, stored);
         if (!walk.left) break;
         __syncthreads();                                // every wave has read what it put into the second buffer
     }

@@ -148,6 +148,65 @@ __global__ __launch_bounds__(256) void k_mx_quantize(MxQuantArgs a, uint32_t col
     }
 }
 
+// The rows form of tokens sorted by expert, rounded to nearest and without weights: every slot of a token holds the same codes.  So a
+// token's row is read and quantised once and written to its choices' slots, and further workgroups, 32 slots each, fill the empty
+// ones with zeros.
+constexpr int kFillSlots = 32;
+template <int RPT>
+__global__ __launch_bounds__(256) void k_mx_quantize_tokens(MxQuantArgs a, uint32_t col_tiles, uint32_t token_groups) {
+    const int t = threadIdx.x;
+    const MxOperand o = a.out;
+    const uint32_t zero_byte = mx_scale_byte(0u, a.ceil_rule != 0);
+    const int64_t blocks = (a.cols + kMxBlock - 1) / kMxBlock;
+    if (blockIdx.x >= token_groups) {
+        const int64_t slot0 = (int64_t)(blockIdx.x - token_groups) * kFillSlots + t / 64 * (kFillSlots / 4);
+        for (int i = 0; i < kFillSlots / 4; ++i) {
+            const int64_t slot = slot0 + i;
+            if (slot >= a.rows || (uint32_t)a.src[slot] < a.choices) continue;
+            for (int64_t b = t % 64; b < blocks; b += 64) {
+                *reinterpret_cast<u32x4*>(o.codes + slot * o.ld + b * 16) = u32x4{0u, 0u, 0u, 0u};
+                o.scales[slot * o.ld_s + b] = (uint8_t)zero_byte;
+            }
+        }
+        return;
+    }
+    const uint32_t ct = blockIdx.x % col_tiles;
+    const int64_t c = (int64_t)ct * kTileCols + (t & 15) * 8, block = c / kMxBlock;
+    const int64_t token0 = (int64_t)(blockIdx.x / col_tiles) * (RPT * 16) + (t >> 4);
+    const uint32_t tokens = a.choices / a.top_k;
+    constexpr uint32_t kAtOnce = 2;                     // slots on their way with the rows
+    u32x4 v[RPT];
+    uint32_t slots[RPT][kAtOnce];
+#pragma unroll
+    for (int i = 0; i < RPT; ++i) {
+        const int64_t token = token0 + 16 * i;
+        v[i] = token < tokens && c < a.cols ? load8(a.x + token * a.ld, c, a.cols) : u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+        for (uint32_t j = 0; j < kAtOnce; ++j)
+            slots[i][j] = token < tokens && j < a.top_k ? (uint32_t)a.slot_of[token * a.top_k + j] : ~0u;
+    }
+#pragma unroll
+    for (int i = 0; i < RPT; ++i) {
+        const int64_t token = token0 + 16 * i;
+        uint32_t m = 0u;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) m = pk_max_u16(m, v[i][j] & 0x7FFF7FFFu);
+        uint32_t amax = fold_max16(m) << 16;
+        amax = max(amax, (uint32_t)__shfl_xor((int)amax, 1));
+        amax = max(amax, (uint32_t)__shfl_xor((int)amax, 2));
+        const uint32_t byte = mx_scale_byte(amax, a.ceil_rule != 0), codes = mx_codes8_nearest(v[i], byte);
+        if (token >= tokens || block >= blocks) continue;
+        auto put = [&](uint32_t slot) {
+            if (slot >= (uint64_t)a.rows) return;
+            *reinterpret_cast<uint32_t*>(o.codes + slot * o.ld + (c >> 1)) = codes;
+            if ((t & 3) == 0) o.scales[slot * o.ld_s + block] = (uint8_t)byte;
+        };
+#pragma unroll
+        for (uint32_t j = 0; j < kAtOnce; ++j) put(slots[i][j]);
+        for (uint32_t j = kAtOnce; j < a.top_k; ++j) put((uint32_t)a.slot_of[token * a.top_k + j]);
+    }
+}
+
 // Eight codes to eight BF16 values per lane, RPT rows of them; every value is exact.
 template <int RPT, bool STREAM>
 __global__ __launch_bounds__(256) void k_mx_dequantize(int64_t rows, int64_t cols, MxOperand op, uint16_t* y, int64_t ld_y, int64_t batch_y,
@@ -197,6 +256,14 @@ hipError_t launch_mx_quantize(const MxQuantArgs& a, hipStream_t st) {
     const bool rows_form = a.out.codes != nullptr, t_form = a.out_t.codes != nullptr;
     const bool tall = a.rows * a.cols > kManyElements;
     const int tile_rows = t_form ? 128 : tall ? 32 : 16;
+    if (a.src && !t_form && !a.weights && !a.stochastic) {
+        const int64_t groups = ((int64_t)(a.choices / a.top_k) + tile_rows - 1) / tile_rows * col_tiles, fill = (a.rows + kFillSlots - 1) / kFillSlots;
+        if (groups + fill > 0x7FFFFFFFll) return hipErrorInvalidValue;
+        const dim3 grid((uint32_t)(groups + fill));
+        if (tall) k_mx_quantize_tokens<2><<<grid, dim3(256), 0, st>>>(a, col_tiles, (uint32_t)groups);
+        else k_mx_quantize_tokens<1><<<grid, dim3(256), 0, st>>>(a, col_tiles, (uint32_t)groups);
+        return hipGetLastError();
+    }
     const int64_t tiles = ((a.rows + tile_rows - 1) / tile_rows) * col_tiles;
     if (tiles > 0x7FFFFFFFll) return hipErrorInvalidValue;
     const dim3 grid((uint32_t)tiles, 1, (uint32_t)a.batch);
