@@ -49,7 +49,8 @@ typedef struct mor_mx_operand {
     uint8_t* codes;        /* 16-byte aligned */
     int64_t  ld_codes;     /* bytes, multiple of 16, >= 16 * ceil(cols / 32) */
     uint8_t* scales;       /* 4-byte aligned */
-    int64_t  ld_scales;    /* bytes, multiple of 4, >= ceil(cols / 32) */
+    int64_t  ld_scales;    /* bytes, multiple of 4, >= ceil(cols / 32); a product reads a row's bytes up to the next multiple of 4,
+                              whatever stands there */
     int64_t  batch_codes;  /* bytes between the operands of a batch, multiple of 16 (ignored for one operand) */
     int64_t  batch_scales; /* the same of the scales, multiple of 4 */
 } mor_mx_operand;

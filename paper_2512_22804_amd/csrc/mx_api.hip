@@ -36,7 +36,7 @@ mor_status check_order(const mor_expert_order* o) {
     if (!o) return MOR_ERR_NULL;
     const int64_t need = mor_expert_capacity(o->tokens, o->top_k, o->n_experts, o->align);
     if (need < 0 || o->capacity < need || o->capacity % o->align || o->reserved != 0) return MOR_ERR_SHAPE;
-    if (!o->offsets || (o->tokens > 0 && (!o->slot_of || !o->src))) return MOR_ERR_NULL;
+    if (!o->offsets || (o->tokens > 0 && !o->slot_of) || (o->capacity > 0 && !o->src)) return MOR_ERR_NULL;
     if (!aligned(o->offsets, 4) || !aligned(o->slot_of, 4) || !aligned(o->src, 4)) return MOR_ERR_ALIGN;
     return MOR_OK;
 }

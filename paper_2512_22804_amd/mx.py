@@ -99,7 +99,7 @@ def _vector(t: torch.Tensor | None, name: str, dtype, n: int) -> None:
         raise ValueError(f"{name} must be {n} contiguous elements of {dtype} in device memory")
 
 
-@dataclass
+@dataclass(frozen=True)
 class MxOperand:
     """A 4-bit operand of ``rows`` x ``cols`` elements, or a batch of them (three-dimensional tensors)."""
     codes: torch.Tensor     # ([batch,] rows, 16 * blocks or more) uint8, two codes per byte
@@ -116,10 +116,9 @@ class MxOperand:
         if self.codes.device != self.scales.device:
             raise ValueError("codes and scales must live on one device")
         lone = self.rows == 1
-        self._struct = MorMxOperand(self.codes.data_ptr(), self.codes.shape[-1] if lone else self.codes.stride(-2), self.scales.data_ptr(),
-                                    self.scales.shape[-1] if lone else self.scales.stride(-2),
-                                    self.codes.stride(0) if self.codes.dim() == 3 else 0,
-                                    self.scales.stride(0) if self.scales.dim() == 3 else 0)
+        object.__setattr__(self, "_struct", MorMxOperand(
+            None, self.codes.shape[-1] if lone else self.codes.stride(-2), None, self.scales.shape[-1] if lone else self.scales.stride(-2),
+            self.codes.stride(0) if self.codes.dim() == 3 else 0, self.scales.stride(0) if self.scales.dim() == 3 else 0))
 
     @property
     def blocks(self) -> int:
@@ -132,7 +131,9 @@ class MxOperand:
     def struct(self) -> MorMxOperand:
         if not self.codes.is_cuda:
             raise ValueError("the operand must live in device memory")
-        return self._struct
+        struct = self._struct
+        struct.codes, struct.scales = self.codes.data_ptr(), self.scales.data_ptr()
+        return struct
 
 
 def alloc_operand(rows: int, cols: int, device, batch: int | None = None) -> MxOperand:
@@ -142,7 +143,7 @@ def alloc_operand(rows: int, cols: int, device, batch: int | None = None) -> MxO
                      torch.empty((*lead, -(-blocks // 4) * 4), dtype=torch.uint8, device=device), rows, cols)
 
 
-@dataclass
+@dataclass(frozen=True)
 class ExpertOrder:
     """Tokens sorted by expert: buffers that :func:`mor_expert_sort` fills and the other calls read."""
     tokens: int
@@ -159,11 +160,12 @@ class ExpertOrder:
         _vector(self.offsets, "offsets", torch.int32, self.n_experts + 1)
         _vector(self.slot_of, "slot_of", torch.int32, self.tokens * self.top_k)
         _vector(self.src, "src", torch.int32, self.capacity)
-        self._struct = MorExpertOrder(self.tokens, self.top_k, self.n_experts, self.align, self.capacity, 0, self.offsets.data_ptr(),
-                                      self.slot_of.data_ptr(), self.src.data_ptr())
+        object.__setattr__(self, "_struct", MorExpertOrder(self.tokens, self.top_k, self.n_experts, self.align, self.capacity, 0))
 
     def struct(self) -> MorExpertOrder:
-        return self._struct
+        struct = self._struct
+        struct.offsets, struct.slot_of, struct.src = self.offsets.data_ptr(), self.slot_of.data_ptr(), self.src.data_ptr()
+        return struct
 
 
 def expert_capacity(tokens: int, top_k: int, n_experts: int, align: int = 128) -> int:
