@@ -68,6 +68,20 @@ __device__ __forceinline__ bool find_rows(const MxProductArgs& p, uint32_t index
     return false;
 }
 
+// How many tiles that makes.
+__device__ __forceinline__ uint32_t count_rows(const MxProductArgs& p, int height) {
+    const int lane = threadIdx.x & 63;
+    uint32_t tiles = 0u;
+    for (int e = lane; e < p.n_experts; e += 64) {
+        int64_t lo, hi;
+        segment(p.offsets, e, p.m, &lo, &hi);
+        tiles += (uint32_t)((hi - lo + height - 1) / height);
+    }
+#pragma unroll
+    for (int d = 32; d; d >>= 1) tiles += (uint32_t)__shfl_xor((int)tiles, d);
+    return (uint32_t)__builtin_amdgcn_readfirstlane((int)tiles);
+}
+
 template <int MODE>
 __device__ __forceinline__ bool find_tile(const MxProductArgs& p, uint32_t m_tile, uint32_t z, int height, Tile* tile) {
     tile->k0 = 0;
@@ -455,15 +469,30 @@ __device__ __forceinline__ void make_uniform(TileWork<S>* w) {
 }
 
 // The tiles of a workgroup, one after the other.  The XCDs take the workgroups in turn; each gets a run of tiles, in patches of 8
-// tile rows, so that the tiles at work together share their operands in its L2.
+// tile rows, so that the tiles at work together share their operands in its L2.  The experts' results, whose depths differ, are dealt
+// out in shorter runs, an eighth of an expert's each: otherwise the XCD with the longest depths finishes last.
 struct Walk {
-    uint32_t left;                      // tiles of this XCD's run from the present one on
+    uint32_t left;                      // tiles of this XCD from the present one on
     uint32_t z, patch, in_patch;        // expert or part, patch, tile in it
     uint32_t n_tiles, m_tiles, stride;
-    __device__ __forceinline__ Walk(uint32_t total, uint32_t mt, uint32_t nt, bool many) {
-        const uint32_t x = blockIdx.x % 8, run = total / 8 + (x < total % 8 ? 1u : 0u);
-        uint32_t id = x * (total / 8) + min(x, total % 8) + blockIdx.x / 8;
-        left = run > blockIdx.x / 8 ? run - blockIdx.x / 8 : 0u;
+    uint32_t run, in_run;               // tiles of a run, which one of them
+    __device__ __forceinline__ Walk(uint32_t total, uint32_t mt, uint32_t nt, bool many, bool shorter) {
+        const uint32_t x = blockIdx.x % 8, first = blockIdx.x / 8;
+        uint32_t id, mine;
+        if (shorter) {
+            run = max(mt * nt / 8, 1u);
+            const uint32_t runs = total / run, rest = total - runs * run, full = runs / 8 + (x < runs % 8 ? 1u : 0u);
+            mine = full * run + (x == runs % 8 ? rest : 0u);
+            id = ((first / run) * 8 + x) * run;
+            in_run = first % run;
+            id += in_run;
+        } else {
+            run = ~0u;
+            in_run = 0u;
+            mine = total / 8 + (x < total % 8 ? 1u : 0u);
+            id = x * (total / 8) + min(x, total % 8) + first;
+        }
+        left = mine > first ? mine - first : 0u;
         n_tiles = nt; m_tiles = mt;
         stride = (gridDim.x - x + 7) / 8;       // workgroups of this XCD
         z = many ? id / (mt * nt) : 0u;
@@ -471,10 +500,12 @@ struct Walk {
         patch = id / (8 * nt);
         in_patch = id - patch * (8 * nt);
     }
-    __device__ __forceinline__ void next(bool many) {
+    __device__ __forceinline__ void next(bool many, bool shorter) {
         left = left > stride ? left - stride : 0u;
         in_patch += stride;
-        for (;;) {                      // a few times at most: patches hold 8 n_tiles tiles, the last one of an expert fewer
+        if (shorter)
+            for (in_run += stride; in_run >= run; in_run -= run) in_patch += 7 * run;    // the runs of the other XCDs
+        for (;;) {                      // patches hold 8 n_tiles tiles, the last one of an expert fewer
             const uint32_t size = min(8u, m_tiles - patch * 8) * n_tiles;
             if (in_patch < size || !left) break;
             in_patch -= size;
@@ -541,9 +572,12 @@ __global__ __launch_bounds__(256, GROUPS) void k_mx_tile(MxProductArgs p, uint32
     const uint8_t* lds_scales = lds + S::kScalesAt;
 
     TileWork<S> w;
-    Walk walk(total, m_tiles, n_tiles, MODE != kMxRows);
-    while (walk.left && !find_work<MODE, BM, BN>(p, walk, lane, wave, &w)) walk.next(MODE != kMxRows);
-    if (!walk.left) return;
+    if (MODE == kMxRows) {                              // the host knows no more than a bound of it
+        m_tiles = count_rows(p, BM);
+        total = m_tiles * n_tiles;
+    }
+    Walk walk(total, m_tiles, n_tiles, MODE != kMxRows, MODE == kMxDepth);
+    if (!walk.left || !find_work<MODE, BM, BN>(p, walk, lane, wave, &w)) return;
     make_uniform(&w);
     request_scales<S>(lds_at + S::kScalesAt, w.q, 0, wave);
 #pragma unroll
@@ -591,8 +625,8 @@ __global__ __launch_bounds__(256, GROUPS) void k_mx_tile(MxProductArgs p, uint32
         }
         // this tile's place in C, then the next tile
         const int64_t base = MODE != kMxRows ? w.t.expert * p.batch_c : 0, m0 = w.t.m0 + wm, m_end = w.t.m_end, n0 = w.n0 + wn;
-        do walk.next(MODE != kMxRows);
-        while (walk.left && !find_work<MODE, BM, BN>(p, walk, lane, wave, &w));
+        walk.next(MODE != kMxRows, MODE == kMxDepth);
+        if (walk.left) find_work<MODE, BM, BN>(p, walk, lane, wave, &w);
         __builtin_amdgcn_s_waitcnt(0x0070);             // the empty requests too, before the buffers are written; the last reads
         __syncthreads();
         if (walk.left) {
