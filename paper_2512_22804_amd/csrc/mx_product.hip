@@ -472,33 +472,36 @@ __device__ __forceinline__ void make_uniform(TileWork<S>* w) {
 // tile rows, so that the tiles at work together share their operands in its L2.  The experts' results, whose depths differ, are dealt
 // out in shorter runs, an eighth of an expert's each: otherwise the XCD with the longest depths finishes last.
 struct Walk {
-    uint32_t left;                      // tiles of this XCD from the present one on
+    uint32_t left;                      // tiles (or pieces) of this workgroup's XCD from the present one on
     uint32_t z, patch, in_patch;        // expert or part, patch, tile in it
-    uint32_t n_tiles, m_tiles, stride;
+    uint32_t n_tiles, m_tiles, total;
+    uint32_t x, first, stride;          // XCD, which of its workgroups this is, how many it has
     uint32_t run, in_run;               // tiles of a run, which one of them
-    __device__ __forceinline__ Walk(uint32_t total, uint32_t mt, uint32_t nt, bool many, bool shorter) {
-        const uint32_t x = blockIdx.x % 8, first = blockIdx.x / 8;
-        uint32_t id, mine;
+    uint32_t mine;                      // tiles of this XCD
+    __device__ __forceinline__ Walk(uint32_t all, uint32_t mt, uint32_t nt, bool shorter) {
+        total = all; n_tiles = nt; m_tiles = mt;
+        x = blockIdx.x % 8;
+        first = blockIdx.x / 8;
+        stride = (gridDim.x - x + 7) / 8;
+        run = shorter ? max(mt * nt / 8, 1u) : ~0u;
+        mine = total / 8 + (x < total % 8 ? 1u : 0u);
         if (shorter) {
-            run = max(mt * nt / 8, 1u);
-            const uint32_t runs = total / run, rest = total - runs * run, full = runs / 8 + (x < runs % 8 ? 1u : 0u);
-            mine = full * run + (x == runs % 8 ? rest : 0u);
-            id = ((first / run) * 8 + x) * run;
-            in_run = first % run;
-            id += in_run;
-        } else {
-            run = ~0u;
-            in_run = 0u;
-            mine = total / 8 + (x < total % 8 ? 1u : 0u);
-            id = x * (total / 8) + min(x, total % 8) + first;
+            const uint32_t runs = total / run;
+            mine = (runs / 8 + (x < runs % 8 ? 1u : 0u)) * run + (x == runs % 8 ? total - runs * run : 0u);
         }
-        left = mine > first ? mine - first : 0u;
-        n_tiles = nt; m_tiles = mt;
-        stride = (gridDim.x - x + 7) / 8;       // workgroups of this XCD
-        z = many ? id / (mt * nt) : 0u;
-        id -= z * (mt * nt);
-        patch = id / (8 * nt);
-        in_patch = id - patch * (8 * nt);
+    }
+    // The XCD's tile number `at`.
+    __device__ __forceinline__ void place(uint32_t at, bool many, bool shorter) {
+        uint32_t id = x * (total / 8) + min(x, total % 8) + at;
+        in_run = at;
+        if (shorter) {
+            in_run = at % run;
+            id = (at / run * 8 + x) * run + in_run;
+        }
+        z = many ? id / (m_tiles * n_tiles) : 0u;
+        id -= z * (m_tiles * n_tiles);
+        patch = id / (8 * n_tiles);
+        in_patch = id - patch * (8 * n_tiles);
     }
     __device__ __forceinline__ void next(bool many, bool shorter) {
         left = left > stride ? left - stride : 0u;
@@ -514,14 +517,20 @@ struct Walk {
     }
 };
 
-template <int MODE, int BM, int BN, class S>
-__device__ __forceinline__ bool find_work(const MxProductArgs& p, const Walk& walk, int lane, int wave, TileWork<S>* w) {
+// What the walk's present tile needs, or the quarter `piece` of a tile of twice the size (QUARTERS); false: nothing.
+template <int MODE, int BM, int BN, bool QUARTERS, class S>
+__device__ __forceinline__ bool find_work(const MxProductArgs& p, const Walk& walk, uint32_t piece_of, int lane, int wave, TileWork<S>* w) {
     const uint32_t tall = min(8u, walk.m_tiles - walk.patch * 8), z = walk.z;
     uint32_t in_patch = walk.in_patch;
     const uint32_t n_tile = tall == 8 ? in_patch / 8 : in_patch / tall, m_tile = walk.patch * 8 + (in_patch - n_tile * tall);
     Tile& t = w->t;
-    if (!find_tile<MODE>(p, m_tile, z, BM, &t)) return false;
-    w->n0 = (int64_t)n_tile * BN;
+    if (!find_tile<MODE>(p, m_tile, z, QUARTERS ? 2 * BM : BM, &t)) return false;
+    w->n0 = (int64_t)n_tile * (QUARTERS ? 2 * BN : BN);
+    if (QUARTERS) {
+        t.m0 += (piece_of & 1) * BM;
+        w->n0 += (piece_of >> 1) * BN;
+        if (!__builtin_amdgcn_readfirstlane(t.m0 < t.m_end && w->n0 < p.n)) return false;
+    }
     w->blocks = __builtin_amdgcn_readfirstlane(t.k_end - t.k0);
     w->stages = max((w->blocks + 7) / 8, 1);             // (no depth at all: one stage of zeros)
     const int64_t row_bytes = (int64_t)p.blocks * 16, row_scales = ((int64_t)p.blocks + 3) & ~3ll;
@@ -548,13 +557,12 @@ __device__ __forceinline__ bool find_work(const MxProductArgs& p, const Walk& wa
 
 // Workgroups stay and take tile after tile: the next tile's first stage is on its way while the sums go out by way of the second
 // buffer.
-template <int MODE, bool F32, int BM, int BN, int GROUPS>
-__global__ __launch_bounds__(256, GROUPS) void k_mx_tile(MxProductArgs p, uint32_t total, uint32_t m_tiles, uint32_t n_tiles) {
+template <int MODE, bool F32, int BM, int BN, bool QUARTERS>
+__device__ __forceinline__ void take_tiles(const MxProductArgs& p, Walk& walk, uint8_t* lds, uint32_t done) {
     typedef TileShape<BM, BN> S;
     constexpr int FM = S::FM, FN = S::FN;
     constexpr int kStores = FM * FN * 32 * 32 * (F32 ? 4 : 2) / 1024;           // of a wave's tile in whole rows
     constexpr int kAfterStores = kStores + S::kFirstRequests < 63 ? kStores + S::kFirstRequests : 63;
-    __shared__ __align__(1024) uint8_t lds[S::kLds];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int row = lane & 31;
     const uint32_t half = lane >> 5;
@@ -572,12 +580,17 @@ __global__ __launch_bounds__(256, GROUPS) void k_mx_tile(MxProductArgs p, uint32
     const uint8_t* lds_scales = lds + S::kScalesAt;
 
     TileWork<S> w;
-    if (MODE == kMxRows) {                              // the host knows no more than a bound of it
-        m_tiles = count_rows(p, BM);
-        total = m_tiles * n_tiles;
-    }
-    Walk walk(total, m_tiles, n_tiles, MODE != kMxRows, MODE == kMxDepth);
-    if (!walk.left || !find_work<MODE, BM, BN>(p, walk, lane, wave, &w)) return;
+    // this workgroup's first piece, the next one that is there
+    uint32_t piece = walk.first;
+    auto find = [&]() {
+        if (!QUARTERS) return find_work<MODE, BM, BN, false>(p, walk, 0u, lane, wave, &w);
+        for (; walk.left; piece += walk.stride, walk.left = walk.left > walk.stride ? walk.left - walk.stride : 0u) {
+            walk.place(done + piece / 4, MODE != kMxRows, MODE == kMxDepth);
+            if (find_work<MODE, BM, BN, true>(p, walk, piece % 4, lane, wave, &w)) return true;
+        }
+        return false;
+    };
+    if (!find()) return;
     make_uniform(&w);
     request_scales<S>(lds_at + S::kScalesAt, w.q, 0, wave);
 #pragma unroll
@@ -606,7 +619,8 @@ __global__ __launch_bounds__(256, GROUPS) void k_mx_tile(MxProductArgs p, uint32
             for (int j = 0; j < FN; ++j) sc.b[j] = mask(*reinterpret_cast<const u32x2*>(lds_scales + at.sb + j * 512));
         }
         uint32_t cur = 0u;                              // buffer of the stage
-        for (int s = 0; s < w.stages; ++s) {
+        int s = 0;
+        do {                                            // one stage at least
             const uint8_t *here = lds + cur, *there = lds + (S::kCodes - cur);
             // the next stage's scales: pairs of stages take turns in two buffers
             const uint8_t* sc_next = lds_scales + ((s + 1) >> 1 & 1) * S::kScales + ((s + 1) & 1) * 8;
@@ -622,11 +636,16 @@ __global__ __launch_bounds__(256, GROUPS) void k_mx_tile(MxProductArgs p, uint32
             multiply_step<3, S>(acc, f1, f0, sc, fresh, there + at.a[0], there + at.b[0], sc_next + at.sa, sc_next + at.sb, to_here, w.q, s + 2, wave, mask);
             sc = fresh;
             cur = S::kCodes - cur;
-        }
+        } while (++s < w.stages);
         // this tile's place in C, then the next tile
         const int64_t base = MODE != kMxRows ? w.t.expert * p.batch_c : 0, m0 = w.t.m0 + wm, m_end = w.t.m_end, n0 = w.n0 + wn;
-        walk.next(MODE != kMxRows, MODE == kMxDepth);
-        if (walk.left) find_work<MODE, BM, BN>(p, walk, lane, wave, &w);
+        if (QUARTERS) {
+            piece += walk.stride;
+            walk.left = walk.left > walk.stride ? walk.left - walk.stride : 0u;
+        } else {
+            walk.next(MODE != kMxRows, MODE == kMxDepth);
+        }
+        if (walk.left) find();
         __builtin_amdgcn_s_waitcnt(0x0070);             // the empty requests too, before the buffers are written; the last reads
         __syncthreads();
         if (walk.left) {
@@ -642,6 +661,34 @@ __global__ __launch_bounds__(256, GROUPS) void k_mx_tile(MxProductArgs p, uint32
         store_tile<F32, FM, FN, S::kCodes / 4, MODE == kMxDepth ? kBufStoreAux : 0>(p, lds + S::kCodes + wave * (S::kCodes / 4), acc, base, m0, m_end, n0, own_lane, stored);
         if (!walk.left) break;
         __syncthreads();                                // every wave has read what it put into the second buffer
+    }
+}
+
+// An XCD's workgroups take its tiles round by round.  If few are left for the last round (a quarter of the workgroups' number at most),
+// these are cut in quarters, one for each: 128 x 128 elements take 0.3 times as long as 256 x 256 (16384 rows of 16 experts, 2048 x 4096,
+// 2.25 rounds: 90 us, 102 without; two quarters for each would be slower than whole tiles for half of them: 6144 x 4096 x 8192,
+// 1.5 rounds: 126 us and 120).
+template <int MODE, bool F32, int BM, int BN, int GROUPS>
+__global__ __launch_bounds__(256, GROUPS) void k_mx_tile(MxProductArgs p, uint32_t total, uint32_t m_tiles, uint32_t n_tiles) {
+    constexpr bool kQuarters = GROUPS == 1;
+    __shared__ __align__(1024) uint8_t lds[TileShape<BM, BN>::kLds];
+    if (MODE == kMxRows) {                              // the host knows no more than a bound of it
+        m_tiles = count_rows(p, BM);
+        total = m_tiles * n_tiles;
+    }
+    Walk walk(total, m_tiles, n_tiles, MODE == kMxDepth);
+    uint32_t rest = kQuarters ? walk.mine % walk.stride : 0u;
+    if (rest * 4 > walk.stride) rest = 0u;
+    const uint32_t whole = walk.mine - rest;
+    if (whole > walk.first) {
+        walk.left = whole - walk.first;
+        walk.place(walk.first, MODE != kMxRows, MODE == kMxDepth);
+        take_tiles<MODE, F32, BM, BN, false>(p, walk, lds, 0u);
+    }
+    if (kQuarters && rest * 4 > walk.first) {
+        __syncthreads();
+        walk.left = rest * 4 - walk.first;
+        take_tiles<MODE, F32, BM / 2, BN / 2, true>(p, walk, lds, whole);
     }
 }
 
@@ -752,7 +799,9 @@ static ProductPlan plan_product(int mode, int64_t m, int64_t n, int64_t blocks, 
     const int64_t batch = mode == kMxDepth ? experts : 1;
     const int64_t large = ((m + 255) / 256) * ((n + 255) / 256) * batch, small = ((m + 127) / 128) * ((n + 127) / 128) * batch;
     const int64_t rest = small % 512;
-    const double in_large = (double)((large + 255) / 256) * (1.9 * stages + 8);
+    const int64_t left = large % 256;
+    const double in_large = (double)(large / 256) * (1.9 * stages + 8) +
+                            (left == 0 ? 0.0 : left > 64 ? 1.9 * stages + 8 : 0.56 * stages + 5);
     const double in_small = (double)(small / 512) * (1.29 * stages + 5) + (rest == 0 ? 0.0 : (rest <= 256 ? 0.56 : 1.29) * stages + 5);
     if (in_large <= in_small) return {ProductPlan::kLargeTiles, 1};
     // Few tiles and a long depth: parts of it on idle CUs.  They are written and read again at about 4 TB/s, and joining them is a
