@@ -786,8 +786,8 @@ __global__ __launch_bounds__(256) void k_mx_join(MxProductArgs p, const float* p
 }  // namespace
 
 // Which kernel a product of a given size takes.  Times in us, measured on whole and partly filled cards: a stage of a 256 x 256 tile
-// 1.9, of two 128 x 128 tiles on a CU 1.29, of one 0.56, and what a tile costs besides 8 and 5.  (8192 x 14336 x 4096: 263 us in
-// large tiles, 322 in small ones; 2048 x 2048 x 2048: 20.4 and 10.3.)
+// 1.9, of two 128 x 128 tiles on a CU 1.29, of one 0.56, and what a tile costs besides 8 and 5.  (In large tiles and in small ones,
+// us: 4096 x 4096 x 4096 38 and 47, 4096 x 5120 x 512 16.8 and 17.4, 2048 x 4096 x 4096 30.1 and 27.6, 1024 x 4096 x 4096 27.9 and 17.1.)
 struct ProductPlan {
     enum { kFew, kSmallTiles, kLargeTiles } kind;
     int splits;                         // parts of the depth
@@ -801,7 +801,7 @@ static ProductPlan plan_product(int mode, int64_t m, int64_t n, int64_t blocks, 
     const int64_t rest = small % 512;
     const int64_t left = large % 256;
     const double in_large = (double)(large / 256) * (1.9 * stages + 8) +
-                            (left == 0 ? 0.0 : left > 64 ? 1.9 * stages + 8 : 0.56 * stages + 5);
+                            (left == 0 ? 0.0 : left > 64 || large < 256 ? 1.9 * stages + 8 : 0.56 * stages + 5);
     const double in_small = (double)(small / 512) * (1.29 * stages + 5) + (rest == 0 ? 0.0 : (rest <= 256 ? 0.56 : 1.29) * stages + 5);
     if (in_large <= in_small) return {ProductPlan::kLargeTiles, 1};
     // Few tiles and a long depth: parts of it on idle CUs.  They are written and read again at about 4 TB/s, and joining them is a
