@@ -9,7 +9,7 @@ namespace {
 
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
 constexpr int kMaxExperts = 1024;       // one lane each
-constexpr int64_t kSortLone = 4096;     // choices that one workgroup sorts alone: 5.9 us for 1332, two launches take 8 and more
+constexpr int64_t kSortLone = 2048;     // choices that one workgroup sorts alone: 5.2 us for 1332, 9.6 for 4000; two launches 7.7
 constexpr int64_t kSortChunks = 256;    // workgroups at most, each of which sums up the counts of all
 
 __device__ __forceinline__ uint32_t expert_of(const int32_t* ids, int64_t i, int64_t n, uint32_t experts) {
@@ -57,6 +57,8 @@ __global__ __launch_bounds__(kSortThreads) void k_expert_place(const int32_t* id
     __shared__ uint8_t in_wave[kSortWaves][kMaxExperts];    // choices of the expert among a wave's 64
     const uint32_t experts = (uint32_t)o.n_experts, e = threadIdx.x, chunks = gridDim.x;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t i0 = (int64_t)blockIdx.x * rounds * kSortThreads;
+    uint32_t id = expert_of(ids, i0 + threadIdx.x, choices, experts);       // the first round's, on its way as early as can be
     uint32_t total = 0u, earlier = 0u;
     if (LONE) {
         if (e <= experts) next[e] = 0u;
@@ -69,12 +71,25 @@ __global__ __launch_bounds__(kSortThreads) void k_expert_place(const int32_t* id
         __syncthreads();
         if (e < experts) total = next[e];
         __syncthreads();
-    } else if (e < experts) {
-        for (uint32_t c = 0; c < chunks; ++c) {
-            const uint32_t n = counts[(int64_t)c * experts + e];
-            if (c < blockIdx.x) earlier += n;
-            total += n;
+    } else {
+        // the counts of all chunks, as many lanes to an expert as there are
+        __shared__ uint32_t sums[2][kMaxExperts];
+        if (e < experts) sums[0][e] = sums[1][e] = 0u;
+        __syncthreads();
+        const uint32_t each = kSortThreads / experts;           // chunks at a time
+        if (e < each * experts) {
+            const uint32_t of = e % experts;
+            uint32_t all = 0u, before = 0u;
+            for (uint32_t c = e / experts; c < chunks; c += each) {
+                const uint32_t n = counts[(int64_t)c * experts + of];
+                if (c < blockIdx.x) before += n;
+                all += n;
+            }
+            if (all) atomicAdd(&sums[0][of], all);
+            if (before) atomicAdd(&sums[1][of], before);
         }
+        __syncthreads();
+        if (e < experts) { total = sums[0][e]; earlier = sums[1][e]; }
     }
     const uint32_t padded = (total + o.align - 1) / o.align * o.align;
     const uint32_t start = scan_before(padded, wave_sums);
@@ -83,22 +98,23 @@ __global__ __launch_bounds__(kSortThreads) void k_expert_place(const int32_t* id
         if (e < experts) o.offsets[e] = (int32_t)start;
         if (e == experts - 1) o.offsets[experts] = (int32_t)(start + padded);
     }
-    // empty slots: those of the experts are shared out lane by lane, those behind the last one over all workgroups
-    if (e < experts && e % chunks == blockIdx.x)
-        for (uint32_t s = start + total; s < start + padded; ++s)
-            if (s < (uint32_t)o.capacity) o.src[s] = -1;
+    // empty slots: a wave for those of an expert, those behind the last one shared out over all workgroups
+    __shared__ uint32_t empty[kMaxExperts][2];
+    if (e < experts) { empty[e][0] = start + total; empty[e][1] = start + padded; }
     __shared__ uint32_t end;
     if (e == experts - 1) end = start + padded;
     __syncthreads();
+    if (o.align > 1)
+        for (uint32_t x = blockIdx.x * kSortWaves + wave; x < experts; x += chunks * kSortWaves)
+            for (uint32_t s = empty[x][0] + lane; s < empty[x][1]; s += 64)
+                if (s < (uint32_t)o.capacity) o.src[s] = -1;
     for (int64_t s = (int64_t)end + blockIdx.x * kSortThreads + threadIdx.x; s < o.capacity; s += (int64_t)chunks * kSortThreads) o.src[s] = -1;
 
-    const int64_t i0 = (int64_t)blockIdx.x * rounds * kSortThreads;
     for (int j = 0; j < rounds; ++j) {
         const int64_t i = i0 + j * kSortThreads + threadIdx.x;
         if (i0 + j * kSortThreads >= choices) break;
-        for (uint32_t q = threadIdx.x; q < kSortWaves * kMaxExperts / 4; q += kSortThreads) reinterpret_cast<uint32_t*>(in_wave)[q] = 0u;
-        __syncthreads();
-        const uint32_t id = expert_of(ids, i, choices, experts);
+        for (uint32_t q = lane; q < (experts + 3) / 4; q += 64) reinterpret_cast<uint32_t*>(in_wave[wave])[q] = 0u;
+        if (j > 0) id = expert_of(ids, i, choices, experts);
         uint64_t same = __ballot(id < experts);
         for (uint32_t bit = 1u; bit < experts; bit <<= 1) {
             const uint64_t set = __ballot((id & bit) != 0u);
@@ -113,6 +129,7 @@ __global__ __launch_bounds__(kSortThreads) void k_expert_place(const int32_t* id
             o.slot_of[i] = (int32_t)slot;
             if (slot < (uint32_t)o.capacity) o.src[slot] = (int32_t)i;
         } else if (i < choices) o.slot_of[i] = -1;
+        if (j + 1 == rounds) break;
         __syncthreads();
         if (e < experts) {
             uint32_t n = 0u;
