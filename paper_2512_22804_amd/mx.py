@@ -47,9 +47,10 @@ def load():
     global _lib
     if _lib is None:
         L = binding.load()
-        ptr, i64, op, order = C.c_void_p, C.c_int64, C.POINTER(MorMxOperand), C.POINTER(MorExpertOrder)
+        ptr, i64 = C.c_void_p, C.c_int64
+        op = order = ptr                # addresses of a MorMxOperand, a MorExpertOrder
         signatures = {
-            "mor_mx_quantize": ([C.POINTER(MorMxParams), ptr, op, op, order, ptr, ptr], C.c_int),
+            "mor_mx_quantize": ([ptr, ptr, op, op, order, ptr, ptr], C.c_int),
             "mor_mx_dequantize": ([i64, i64, i64, op, ptr, i64, i64, ptr], C.c_int),
             "mor_mx_product_workspace_bytes": ([i64, i64, i64], C.c_size_t),
             "mor_mx_product": ([i64, i64, i64, op, op, ptr, i64, C.c_int32, ptr, C.c_size_t, ptr], C.c_int),
@@ -74,18 +75,17 @@ def _check(rc: int, where: str) -> None:
         raise binding.MorError(rc, where)
 
 
-def _matrix(t: torch.Tensor, name: str, types=(torch.bfloat16, torch.int16)) -> None:
+def _matrix(t: torch.Tensor, name: str, types=(torch.bfloat16, torch.int16)) -> int:
+    """Checks a matrix (or a batch of them) and returns the elements between its rows."""
     if not t.is_cuda:
         raise ValueError(f"{name} must live in device memory")
     if t.dtype not in types:
         raise ValueError(f"{name}: {t.dtype} is not one of {types}")
-    if t.dim() not in (2, 3) or (t.shape[-1] > 1 and t.stride(-1) != 1):
+    shape, stride = t.shape, t.stride()
+    if len(shape) not in (2, 3) or (stride[-1] != 1 and shape[-1] > 1):
         raise ValueError(f"{name} must be two- or three-dimensional with unit stride along its rows")
-
-
-def _ld(t: torch.Tensor) -> int:
-    """Elements between rows.  The stride of a dimension of size one can be anything; that row's own length serves."""
-    return t.stride(-2) if t.shape[-2] > 1 else t.shape[-1]
+    # the stride of a dimension of size one can be anything; that row's own length serves
+    return stride[-2] if shape[-2] > 1 else shape[-1]
 
 
 def _batch(t: torch.Tensor) -> tuple[int, int]:
@@ -128,12 +128,13 @@ class MxOperand:
     def batch(self) -> int:
         return self.codes.shape[0] if self.codes.dim() == 3 else 1
 
-    def struct(self) -> MorMxOperand:
+    def struct(self) -> int:
+        """Address of the operand's structure, valid as long as the operand."""
         if not self.codes.is_cuda:
             raise ValueError("the operand must live in device memory")
         struct = self._struct
         struct.codes, struct.scales = self.codes.data_ptr(), self.scales.data_ptr()
-        return struct
+        return C.addressof(struct)
 
 
 def alloc_operand(rows: int, cols: int, device, batch: int | None = None) -> MxOperand:
@@ -162,10 +163,11 @@ class ExpertOrder:
         _vector(self.src, "src", torch.int32, self.capacity)
         object.__setattr__(self, "_struct", MorExpertOrder(self.tokens, self.top_k, self.n_experts, self.align, self.capacity, 0))
 
-    def struct(self) -> MorExpertOrder:
+    def struct(self) -> int:
+        """Address of the order's structure, valid as long as the order."""
         struct = self._struct
         struct.offsets, struct.slot_of, struct.src = self.offsets.data_ptr(), self.slot_of.data_ptr(), self.src.data_ptr()
-        return struct
+        return C.addressof(struct)
 
 
 def expert_capacity(tokens: int, top_k: int, n_experts: int, align: int = 128) -> int:
@@ -188,7 +190,7 @@ def mor_mx_quantize(x: torch.Tensor, out: MxOperand | None = None, out_t: MxOper
                     rounding: str = "nearest", seed: int = 0, order: ExpertOrder | None = None, weights: torch.Tensor | None = None) -> None:
     """Quantise ``x`` ([batch,] rows, cols; BF16, or int16 holding its bits) into ``out`` and / or, transposed, ``out_t``.  With ``order`` the
     rows of the operands are its slots, each times its choice's weight if ``weights`` is given."""
-    _matrix(x, "x")
+    ld = _matrix(x, "x")
     rows, cols = x.shape[-2:]
     batch, batch_x = _batch(x)
     if order is not None:
@@ -199,20 +201,20 @@ def mor_mx_quantize(x: torch.Tensor, out: MxOperand | None = None, out_t: MxOper
     for operand, shape, name in ((out, (slots, cols), "out"), (out_t, (cols, slots), "out_t")):
         if operand is not None and ((operand.rows, operand.cols) != shape or operand.batch != batch):
             raise ValueError(f"{name} must be {batch} operand(s) of {shape[0]} x {shape[1]}")
-    params = MorMxParams(rows, cols, _ld(x), batch, batch_x, SCALE_RULE[scale_rule], ROUNDING[rounding], seed & 0xFFFFFFFFFFFFFFFF)
-    _check(load().mor_mx_quantize(C.byref(params), x.data_ptr(), C.byref(out.struct()) if out is not None else None,
-                                  C.byref(out_t.struct()) if out_t is not None else None,
-                                  C.byref(order.struct()) if order is not None else None, binding._ptr(weights), binding._stream()),
+    params = MorMxParams(rows, cols, ld, batch, batch_x, SCALE_RULE[scale_rule], ROUNDING[rounding], seed & 0xFFFFFFFFFFFFFFFF)
+    _check(load().mor_mx_quantize(C.addressof(params), x.data_ptr(), out.struct() if out is not None else None,
+                                  out_t.struct() if out_t is not None else None,
+                                  order.struct() if order is not None else None, binding._ptr(weights), binding._stream()),
            "mor_mx_quantize")
 
 
 def mor_mx_dequantize(operand: MxOperand, y: torch.Tensor) -> None:
     """``y`` ([batch,] rows, cols; BF16): what the operand stands for."""
-    _matrix(y, "y")
+    ld = _matrix(y, "y")
     batch, batch_y = _batch(y)
-    if tuple(y.shape[-2:]) != (operand.rows, operand.cols) or batch != operand.batch:
+    if y.shape[-2:] != (operand.rows, operand.cols) or batch != operand.batch:
         raise ValueError(f"y must be {operand.batch} matrices of {operand.rows} x {operand.cols}")
-    _check(load().mor_mx_dequantize(operand.rows, operand.cols, batch, C.byref(operand.struct()), y.data_ptr(), _ld(y), batch_y,
+    _check(load().mor_mx_dequantize(operand.rows, operand.cols, batch, operand.struct(), y.data_ptr(), ld, batch_y,
                                     binding._stream()), "mor_mx_dequantize")
 
 
@@ -231,32 +233,32 @@ def alloc_product_workspace(a: MxOperand, b: MxOperand, device) -> torch.Tensor 
 
 def mor_mx_product(a: MxOperand, b: MxOperand, c: torch.Tensor, workspace: torch.Tensor | None = None) -> None:
     """``c`` (a.rows, b.rows; BF16 or float32) = a b^T."""
-    _matrix(c, "c", tuple(_OUT))
-    if a.cols != b.cols or a.batch != 1 or b.batch != 1 or tuple(c.shape) != (a.rows, b.rows):
+    ld = _matrix(c, "c", _OUT)
+    if a.cols != b.cols or a.batch != 1 or b.batch != 1 or c.shape != (a.rows, b.rows):
         raise ValueError(f"shapes do not match: {a.rows} x {a.cols}, {b.rows} x {b.cols}, result {tuple(c.shape)}")
-    _check(load().mor_mx_product(a.rows, b.rows, a.cols, C.byref(a.struct()), C.byref(b.struct()), c.data_ptr(), _ld(c), _OUT[c.dtype],
+    _check(load().mor_mx_product(a.rows, b.rows, a.cols, a.struct(), b.struct(), c.data_ptr(), ld, _OUT[c.dtype],
                                  binding._ptr(workspace), workspace.numel() if workspace is not None else 0, binding._stream()),
            "mor_mx_product")
 
 
 def mor_mx_product_rows(a: MxOperand, b: MxOperand, order: ExpertOrder, c: torch.Tensor) -> None:
     """``c`` (capacity, b.rows): the slots' rows of ``a`` times their expert's operand of the batch ``b``, transposed."""
-    _matrix(c, "c", tuple(_OUT))
-    if a.cols != b.cols or a.batch != 1 or a.rows != order.capacity or b.batch != order.n_experts or tuple(c.shape) != (a.rows, b.rows):
+    ld = _matrix(c, "c", _OUT)
+    if a.cols != b.cols or a.batch != 1 or a.rows != order.capacity or b.batch != order.n_experts or c.shape != (a.rows, b.rows):
         raise ValueError(f"shapes do not match: {a.rows} x {a.cols}, {b.batch} of {b.rows} x {b.cols}, {order.n_experts} experts, "
                          f"{order.capacity} slots, result {tuple(c.shape)}")
-    _check(load().mor_mx_product_rows(b.rows, a.cols, C.byref(a.struct()), C.byref(b.struct()), C.byref(order.struct()), c.data_ptr(), _ld(c),
+    _check(load().mor_mx_product_rows(b.rows, a.cols, a.struct(), b.struct(), order.struct(), c.data_ptr(), ld,
                                       _OUT[c.dtype], binding._stream()), "mor_mx_product_rows")
 
 
 def mor_mx_product_depth(a: MxOperand, b: MxOperand, order: ExpertOrder, c: torch.Tensor) -> None:
     """``c`` (n_experts, a.rows, b.rows): for each expert a b^T summed over its slots, which are the columns of both."""
-    _matrix(c, "c", tuple(_OUT))
+    ld = _matrix(c, "c", _OUT)
     if a.cols != order.capacity or b.cols != order.capacity or a.batch != 1 or b.batch != 1 or \
-            c.dim() != 3 or tuple(c.shape) != (order.n_experts, a.rows, b.rows):
+            c.dim() != 3 or c.shape != (order.n_experts, a.rows, b.rows):
         raise ValueError(f"shapes do not match: {a.rows} x {a.cols}, {b.rows} x {b.cols}, {order.n_experts} experts, "
                          f"{order.capacity} slots, result {tuple(c.shape)}")
-    _check(load().mor_mx_product_depth(a.rows, b.rows, C.byref(a.struct()), C.byref(b.struct()), C.byref(order.struct()), c.data_ptr(), _ld(c),
+    _check(load().mor_mx_product_depth(a.rows, b.rows, a.struct(), b.struct(), order.struct(), c.data_ptr(), ld,
                                        _batch(c)[1], _OUT[c.dtype], binding._stream()), "mor_mx_product_depth")
 
 
@@ -264,47 +266,43 @@ def mor_expert_sort(ids: torch.Tensor, order: ExpertOrder) -> None:
     """``ids`` (tokens, top_k) int32: the expert of each choice; outside [0, n_experts): dropped."""
     _vector(ids, "ids", torch.int32, order.tokens * order.top_k)
     ws = order.workspace
-    _check(load().mor_expert_sort(ids.data_ptr(), C.byref(order.struct()), binding._ptr(ws), ws.numel() if ws is not None else 0,
+    _check(load().mor_expert_sort(ids.data_ptr(), order.struct(), binding._ptr(ws), ws.numel() if ws is not None else 0,
                                   binding._stream()), "mor_expert_sort")
 
 
-def _rows(t: torch.Tensor | None, name: str, rows: int, d: int) -> None:
+def _rows(t: torch.Tensor | None, name: str, rows: int, d: int) -> int:
     if t is None:
-        return
-    _matrix(t, name)
-    if tuple(t.shape) != (rows, d):
+        return 0
+    ld = _matrix(t, name)
+    if t.shape != (rows, d):
         raise ValueError(f"{name} must be {rows} x {d}, not {tuple(t.shape)}")
+    return ld
 
 
 def mor_expert_gather(x: torch.Tensor, order: ExpertOrder, xs: torch.Tensor) -> None:
     """``xs`` (capacity, d): the token's row for every slot, zeros for empty ones."""
     d = x.shape[-1]
-    _rows(x, "x", order.tokens, d)
-    _rows(xs, "xs", order.capacity, d)
-    _check(load().mor_expert_gather(x.data_ptr(), _ld(x), d, C.byref(order.struct()), xs.data_ptr(), _ld(xs), binding._stream()),
+    ld_x, ld_xs = _rows(x, "x", order.tokens, d), _rows(xs, "xs", order.capacity, d)
+    _check(load().mor_expert_gather(x.data_ptr(), ld_x, d, order.struct(), xs.data_ptr(), ld_xs, binding._stream()),
            "mor_expert_gather")
 
 
 def mor_expert_combine(ys: torch.Tensor, order: ExpertOrder, weights: torch.Tensor | None, y: torch.Tensor) -> None:
     """``y`` (tokens, d): weighted sum of each token's rows of ``ys`` (capacity, d)."""
     d = ys.shape[-1]
-    _rows(ys, "ys", order.capacity, d)
-    _rows(y, "y", order.tokens, d)
+    ld_ys, ld_y = _rows(ys, "ys", order.capacity, d), _rows(y, "y", order.tokens, d)
     _vector(weights, "weights", torch.float32, order.tokens * order.top_k)
-    _check(load().mor_expert_combine(ys.data_ptr(), _ld(ys), d, C.byref(order.struct()), binding._ptr(weights), y.data_ptr(), _ld(y),
-                                     binding._stream()), "mor_expert_combine")
+    _check(load().mor_expert_combine(ys.data_ptr(), ld_ys, d, order.struct(), binding._ptr(weights), y.data_ptr(), ld_y, binding._stream()),
+           "mor_expert_combine")
 
 
 def mor_expert_combine_backward(dy: torch.Tensor, ys: torch.Tensor | None, order: ExpertOrder, weights: torch.Tensor | None,
                                 dys: torch.Tensor | None, dweights: torch.Tensor | None) -> None:
     """Gradients of :func:`mor_expert_combine`: ``dys`` (capacity, d) and ``dweights`` (tokens, top_k), either may be None."""
     d = dy.shape[-1]
-    _rows(dy, "dy", order.tokens, d)
-    _rows(ys, "ys", order.capacity, d)
-    _rows(dys, "dys", order.capacity, d)
+    ld_dy, ld_ys, ld_dys = _rows(dy, "dy", order.tokens, d), _rows(ys, "ys", order.capacity, d), _rows(dys, "dys", order.capacity, d)
     _vector(weights, "weights", torch.float32, order.tokens * order.top_k)
     _vector(dweights, "dweights", torch.float32, order.tokens * order.top_k)
-    _check(load().mor_expert_combine_backward(dy.data_ptr(), _ld(dy), binding._ptr(ys), _ld(ys) if ys is not None else 0, d,
-                                              C.byref(order.struct()), binding._ptr(weights), binding._ptr(dys),
-                                              _ld(dys) if dys is not None else 0, binding._ptr(dweights), binding._stream()),
+    _check(load().mor_expert_combine_backward(dy.data_ptr(), ld_dy, binding._ptr(ys), ld_ys, d, order.struct(), binding._ptr(weights),
+                                              binding._ptr(dys), ld_dys, binding._ptr(dweights), binding._stream()),
            "mor_expert_combine_backward")
