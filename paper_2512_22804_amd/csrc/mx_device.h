@@ -48,12 +48,19 @@ __device__ __forceinline__ u32x4 philox(uint32_t c0, uint32_t c1, uint32_t c2, u
 // random bits.  From 1 on a grid value has one mantissa bit, so y = |v| 2^-e rounds up where the 22 bits behind it, plus r 2^6,
 // carry: bit 22 of y's pattern on is the code (plus a constant).  Below 1 the same holds of y 2^23 as a whole number, whose
 // steps are those of the binade below 2.  Whole numbers throughout: floor(y / step + r / 65536) without a rounding of its own.
+//
+// The constant makes the two agree at 1, y 2^23 = 2^23 in either form; below it the pattern is the smaller of the two and both lie
+// below 2^23's, above it the pattern is the smaller too and both lie above: the one wanted is the median of all three.
 constexpr uint32_t kStochasticBase = 2 * (127 - 1) + 2 * 23;
-__device__ __forceinline__ uint32_t mx_code_stochastic(float v, int shift, uint32_t r) {
+template <int HALF>                                                         // of `random`: r
+__device__ __forceinline__ uint32_t mx_code_stochastic(float v, int shift, uint32_t random) {
     const float y = __builtin_amdgcn_ldexpf(__builtin_fabsf(v), shift);     // y 2^23
     const uint32_t whole = (uint32_t)y + (kStochasticBase << 22);
-    const uint32_t w = (y < 0x1p23f ? whole : __float_as_uint(y)) + (r << 6);
-    return min(w >> 22, kStochasticBase + 7u);
+    const uint32_t w = __float_as_uint(__builtin_amdgcn_fmed3f(__uint_as_float(whole), y, 0x1p23f));
+    uint32_t sum;                                                           // w + (r << 6)
+    if (HALF == 0) asm("v_mad_u32_u16 %0, %1, 64, %2" : "=v"(sum) : "v"(random), "v"(w));
+    else asm("v_mad_u32_u16 %0, %1, 64, %2 op_sel:[1,0,0,0]" : "=v"(sum) : "v"(random), "v"(w));
+    return min(sum >> 22, kStochasticBase + 7u);
 }
 
 __device__ __forceinline__ bf16x2 bf16_pair(uint32_t word) { return __builtin_bit_cast(bf16x2, word); }
@@ -79,15 +86,19 @@ __device__ __forceinline__ uint32_t mx_codes8_nearest(const float (&v)[8], uint3
 }
 __device__ __forceinline__ uint32_t mx_codes8_stochastic(const float (&v)[8], uint32_t byte, const u32x4& random) {
     const int shift = 23 + 127 - (int)byte;
-    uint32_t c = 0u - kStochasticBase * 0x11111111u, sign = 0;
+    uint32_t c = 0u - kStochasticBase * 0x11111111u;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const uint32_t word = random[j];
-        c += mx_code_stochastic(v[2 * j], shift, word & 0xFFFFu) << (8 * j);
-        c += mx_code_stochastic(v[2 * j + 1], shift, word >> 16) << (8 * j + 4);
-        sign |= (__float_as_uint(v[2 * j]) >> 31) << (8 * j + 3);
-        sign |= (__float_as_uint(v[2 * j + 1]) >> 31) << (8 * j + 7);
+        c += mx_code_stochastic<0>(v[2 * j], shift, random[j]) << (8 * j);
+        c += mx_code_stochastic<1>(v[2 * j + 1], shift, random[j]) << (8 * j + 4);
     }
+    // the signs: the highest bytes of the even elements and of the odd ones, side by side
+    uint32_t high[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+        high[j] = __builtin_amdgcn_perm(__float_as_uint(v[2 + j]), __float_as_uint(v[j]), 0x0C0C0703u) |
+                  __builtin_amdgcn_perm(__float_as_uint(v[6 + j]), __float_as_uint(v[4 + j]), 0x07030C0Cu);
+    const uint32_t sign = (high[0] >> 4 & 0x08080808u) | (high[1] & 0x80808080u);
     return byte == kMxNan ? 0u : c | sign;
 }
 __device__ __forceinline__ void widen8(const u32x4& raw, float (&v)[8]) {

@@ -14,7 +14,7 @@ constexpr int kTileCols = 128;          // columns of a workgroup's tile: 16 lan
 // lanes fill 64 bytes of an output row.  The rows of row block q are rotated by 16 q dwords: the four row blocks that
 // neighbouring lanes read then lie in different banks.
 template <int RPT, bool ROWS, bool T, bool SR, bool WEIGHTED, bool STREAM>
-__global__ __launch_bounds__(256) void k_mx_quantize(MxQuantArgs a, uint32_t col_tiles) {
+__global__ __launch_bounds__(256, T && WEIGHTED ? 3 : 1) void k_mx_quantize(MxQuantArgs a, uint32_t col_tiles) {
     static_assert(!T || RPT == 8, "the transposed form works on 128 x 128 tiles");
     __shared__ __align__(16) uint32_t tile[T ? 128 * 64 : 4];
     __shared__ __align__(16) float row_weight[WEIGHTED ? RPT * 16 : 1];
