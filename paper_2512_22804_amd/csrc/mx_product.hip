@@ -720,37 +720,46 @@ __global__ __launch_bounds__(kFewWaves * 64) void k_mx_few(MxProductArgs p, uint
 #pragma unroll
         for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{};
     const int groups = (p.blocks + 15) / 16;
-    for (int g = wave; g < groups; g += kFewWaves) {
-        u32x4 av[MT][4], bv[NT][4], sa[MT], sb[NT];
+    struct Group {
+        u32x4 a[MT][4], b[NT][4], sa[MT], sb[NT];
+    };
+    auto load = [&](Group& v, int g) {
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
 #pragma unroll
             for (int s = 0; s < 4; ++s)
-                bv[j][s] = __builtin_amdgcn_raw_buffer_load_b128(rb, (uint32_t)(16 * j + row) * (uint32_t)p.ldb + part * 16 + s * 64, g * 256, 0);
-            sb[j] = __builtin_amdgcn_raw_buffer_load_b128(rbs, (uint32_t)(16 * j + row) * (uint32_t)p.ldb_s, g * 16, 0);
+                v.b[j][s] = __builtin_amdgcn_raw_buffer_load_b128(rb, (uint32_t)(16 * j + row) * (uint32_t)p.ldb + part * 16 + s * 64, g * 256, 0);
+            v.sb[j] = __builtin_amdgcn_raw_buffer_load_b128(rbs, (uint32_t)(16 * j + row) * (uint32_t)p.ldb_s, g * 16, 0);
         }
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
 #pragma unroll
             for (int s = 0; s < 4; ++s)
-                av[i][s] = __builtin_amdgcn_raw_buffer_load_b128(ra, (uint32_t)(16 * i + row) * (uint32_t)p.lda + part * 16 + s * 64, g * 256, 0);
-            sa[i] = __builtin_amdgcn_raw_buffer_load_b128(ras, (uint32_t)(16 * i + row) * (uint32_t)p.lda_s, g * 16, 0);
+                v.a[i][s] = __builtin_amdgcn_raw_buffer_load_b128(ra, (uint32_t)(16 * i + row) * (uint32_t)p.lda + part * 16 + s * 64, g * 256, 0);
+            v.sa[i] = __builtin_amdgcn_raw_buffer_load_b128(ras, (uint32_t)(16 * i + row) * (uint32_t)p.lda_s, g * 16, 0);
         }
+    };
+    auto multiply_group = [&](const Group& v, int g) {
         const bool ragged = g * 16 + 16 > p.blocks;
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
             const bool in = !ragged || g * 16 + s * 4 + part < p.blocks;        // behind the last block: codes 0, scales 2^0
             uint32_t scale_b[NT];
 #pragma unroll
-            for (int j = 0; j < NT; ++j) scale_b[j] = in ? sb[j][s] >> (8 * part) : 127u;
+            for (int j = 0; j < NT; ++j) scale_b[j] = in ? v.sb[j][s] >> (8 * part) : 127u;
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
-                const u32x4 codes = in ? av[i][s] : u32x4{0u, 0u, 0u, 0u};
-                const uint32_t scale_a = in ? sa[i][s] >> (8 * part) : 127u;
+                const u32x4 codes = in ? v.a[i][s] : u32x4{0u, 0u, 0u, 0u};
+                const uint32_t scale_a = in ? v.sa[i][s] >> (8 * part) : 127u;
 #pragma unroll
-                for (int j = 0; j < NT; ++j) acc[i][j] = mfma_mx(bv[j][s], scale_b[j], codes, scale_a, acc[i][j]);
+                for (int j = 0; j < NT; ++j) acc[i][j] = mfma_mx(v.b[j][s], scale_b[j], codes, scale_a, acc[i][j]);
             }
         }
+    };
+    for (int g = wave; g < groups; g += kFewWaves) {
+        Group now;
+        load(now, g);
+        multiply_group(now, g);
     }
 #pragma unroll
     for (int i = 0; i < MT; ++i)
@@ -788,13 +797,19 @@ __global__ __launch_bounds__(256) void k_mx_join(MxProductArgs p, const float* p
 // Which kernel a product of a given size takes.  Times in us, measured on whole and partly filled cards: a stage of a 256 x 256 tile
 // 1.9, of two 128 x 128 tiles on a CU 1.29, of one 0.56, and what a tile costs besides 8 and 5.  (In large tiles and in small ones,
 // us: 4096 x 4096 x 4096 38 and 47, 4096 x 5120 x 512 16.8 and 17.4, 2048 x 4096 x 4096 30.1 and 27.6, 1024 x 4096 x 4096 27.9 and 17.1.)
+constexpr int64_t kFewNarrow = 160;      // workgroups of few rows that the CUs want at least
 struct ProductPlan {
     enum { kFew, kSmallTiles, kLargeTiles } kind;
     int splits;                         // parts of the depth
 };
 static ProductPlan plan_product(int mode, int64_t m, int64_t n, int64_t blocks, int64_t experts) {
-    if (mode == kMxDense && m <= 64) return {ProductPlan::kFew, 1};
-    if (mode == kMxRows && m <= 32 * experts) return {ProductPlan::kFew, 1};
+    // (More than 32 rows and a long depth for few workgroups: parts of the depth are better.  64 x 4096 x 14336: 22.5 us, 18.8 in tiles;
+    // 64 x 4096 x 8192: 15.3 and 17.3.)
+    if (mode == kMxDense && m <= 64 && !(m > 32 && n < kFewNarrow * 32 && blocks > 320)) return {ProductPlan::kFew, 1};
+    // Rows of experts: every expert's matrix is read once in tiles, once for each 16 of its rows otherwise.  (Experts of 2048 x 4096, us
+    // for few rows and in tiles: 64 experts with 2 rows each 48.5 and 55, with 4 60.6 and 59.8, with 16 90 and 62; 8 experts of
+    // 4096 x 4096, too few tiles for the CUs, with 12 rows each 21.4 and 22.2, with 16 24.5 and 22.3.)
+    if (mode == kMxRows && m <= (std::min(m, experts) * ((n + 127) / 128) <= 512 ? 12 : 4) * experts) return {ProductPlan::kFew, 1};
     const double stages = (double)((blocks + 7) / 8);
     const int64_t batch = mode == kMxDepth ? experts : 1;
     const int64_t large = ((m + 255) / 256) * ((n + 255) / 256) * batch, small = ((m + 127) / 128) * ((n + 127) / 128) * batch;
@@ -846,7 +861,7 @@ static hipError_t launch_few(int mode, const MxProductArgs& p, hipStream_t st) {
     if (n_tiles * m_tiles > 0x7FFFFFFFll) return hipErrorInvalidValue;
     const dim3 grid((uint32_t)(n_tiles * m_tiles)), block(kFewWaves * 64);
     if (mode == kMxDense) k_mx_few<kMxDense, MT, NT><<<grid, block, 0, st>>>(p, (uint32_t)n_tiles);
-    else k_mx_few<kMxRows, MT, NT><<<grid, block, 0, st>>>(p, (uint32_t)n_tiles);
+    else if constexpr (MT == 1 && NT <= 2) k_mx_few<kMxRows, MT, NT><<<grid, block, 0, st>>>(p, (uint32_t)n_tiles);
     return hipGetLastError();
 }
 
@@ -865,12 +880,17 @@ hipError_t launch_mx_product(int mode, MxProductArgs p, void* workspace, hipStre
     if (near_rows(p)) {
         const ProductPlan plan = plan_product(mode, p.m, p.n, p.blocks, p.n_experts);
         if (plan.kind == ProductPlan::kFew) {
-            // twice the rows of B per workgroup where that leaves enough workgroups: A's rows are read half as often
-            const bool wide = p.n > 8192;
-            if (mode == kMxRows || p.m <= 4) return launch_few<1, 1>(mode, p, st);
-            if (p.m <= 16) return wide ? launch_few<1, 2>(mode, p, st) : launch_few<1, 1>(mode, p, st);
-            if (p.m <= 32) return wide ? launch_few<2, 2>(mode, p, st) : launch_few<2, 1>(mode, p, st);
-            return wide ? launch_few<4, 2>(mode, p, st) : launch_few<4, 1>(mode, p, st);
+            if (mode == kMxRows) {
+                if (std::min<int64_t>(p.m, p.n_experts) * p.n < kFewNarrow * 32) return launch_few<1, 1>(mode, p, st);
+                return launch_few<1, 2>(mode, p, st);
+            }
+            // The more rows of B a workgroup takes, the less often A's are read (64 x 14336 x 4096: 30.5 us with 16, 18.6 with 32, 14.5
+            // with 64), which counts for little up to four (1 x 14336 x 4096: 8.9, 9.6, 9.6); but the CUs want enough workgroups
+            // (64 x 4096 x 4096: 8.6, 10.0, 13.4).
+            const int wide = p.n < kFewNarrow * 32 || (p.m <= 4 && p.n < kFewNarrow * 128) ? 1 : p.n < kFewNarrow * 64 ? 2 : 4;
+            if (p.m <= 16) return wide == 1 ? launch_few<1, 1>(mode, p, st) : wide == 2 ? launch_few<1, 2>(mode, p, st) : launch_few<1, 4>(mode, p, st);
+            if (p.m <= 32) return wide == 1 ? launch_few<2, 1>(mode, p, st) : wide == 2 ? launch_few<2, 2>(mode, p, st) : launch_few<2, 4>(mode, p, st);
+            return wide == 1 ? launch_few<4, 1>(mode, p, st) : wide == 2 ? launch_few<4, 2>(mode, p, st) : launch_few<4, 4>(mode, p, st);
         }
         if (plan.splits == 1) return launch_all_tiles(mode, p, plan.kind == ProductPlan::kLargeTiles, st);
         MxProductArgs part = p;

@@ -59,3 +59,28 @@ def test_depths_of_experts_of_all_sizes(tokens, top_k, experts, m, n, skew):
     for e in range(experts):
         s = slice(starts[e], starts[e + 1])
         close(got[e], av[:, s], bv[:, s], True, starts[e + 1] - starts[e])
+
+
+# few rows against many, 16, 32 or 64 of them to a workgroup; more than 32 rows and a long depth
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("m, n, k", [(3, 20500, 96), (4, 20481, 33), (5, 10300, 130), (16, 5200, 700), (20, 10250, 96), (32, 5203, 1030), (40, 10245, 200),
+                                     (64, 6001, 513), (33, 100, 10400), (64, 3001, 10300), (64, 300, 10240)])
+def test_few_rows(m, n, k, dtype):
+    a, av = random_operand(m, k, 9, spread=3)
+    b, bv = random_operand(n, k, 10, spread=3)
+    close(product(a, b, dtype), av, bv, dtype == torch.float32, k)
+
+
+@pytest.mark.parametrize("tokens, top_k, experts, n, k", [(5, 2, 6, 2100, 140), (1, 2, 30, 5201, 64), (60, 1, 5, 2045, 520), (30, 3, 8, 700, 1100), (63, 1, 5, 300, 96)])
+def test_few_rows_of_experts(tokens, top_k, experts, n, k):
+    order = make_order(skewed(tokens, top_k, experts, "falling", 11), experts, 1)
+    starts = order.offsets.cpu().numpy()
+    a, av = random_operand(order.capacity, k, 12, spread=3)
+    b, bv = random_operand(n, k, 13, batch=experts, spread=3)
+    c = torch.full((order.capacity + 1, n), 7.0, device=DEV)
+    mx.mor_mx_product_rows(a, b, order, c[:-1])
+    got = c.double().cpu().numpy()
+    assert (got[-1] == 7.0).all()
+    for e in range(experts):
+        s = slice(starts[e], starts[e + 1])
+        close(got[s], av[s], bv[e], True, k)
