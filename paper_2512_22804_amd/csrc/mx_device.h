@@ -111,8 +111,11 @@ __device__ __forceinline__ void widen8(const u32x4& raw, float (&v)[8]) {
 
 
 // Eight elements of a BF16 row from column c on; the last ones of a row may be missing and read as zeros.  Rows may start at any
-// element: the wide accesses need no more than the elements' own alignment.
+// element: the wide accesses need no more than the elements' own alignment.  The last elements of a row come with one access too, of
+// the row's last eight, moved down: one at a time, each waits for its own (rows of 1358 elements: 10.8 us instead of XXX).
 typedef u32x4 u32x4_anywhere __attribute__((aligned(2)));
+typedef u32x2 u32x2_anywhere __attribute__((aligned(2)));
+typedef uint32_t u32_anywhere __attribute__((aligned(2)));
 template <bool STREAM = false>
 __device__ __forceinline__ u32x4 load8(const uint16_t* row, int64_t c, int64_t cols) {
     if (c + 8 <= cols) {
@@ -120,8 +123,16 @@ __device__ __forceinline__ u32x4 load8(const uint16_t* row, int64_t c, int64_t c
         return STREAM ? __builtin_nontemporal_load(p) : *p;
     }
     u32x4 v{0u, 0u, 0u, 0u};
-    for (int j = 0; j < 8; ++j)
-        if (c + j < cols) v[j >> 1] |= (uint32_t)row[c + j] << (16 * (j & 1));
+    if (cols >= 8) {
+        const u32x4 last = *reinterpret_cast<const u32x4_anywhere*>(row + cols - 8);
+        const int bits = 16 * (int)(c + 8 - cols);          // 16 .. 112
+        const uint64_t low = ((uint64_t)last[1] << 32) | last[0], high = ((uint64_t)last[3] << 32) | last[2];
+        const uint64_t first = bits >= 64 ? high >> (bits - 64) : (low >> bits) | (high << (64 - bits)), second = bits >= 64 ? 0u : high >> bits;
+        v = u32x4{(uint32_t)first, (uint32_t)(first >> 32), (uint32_t)second, (uint32_t)(second >> 32)};
+    } else {
+        for (int j = 0; j < 8; ++j)
+            if (c + j < cols) v[j >> 1] |= (uint32_t)row[c + j] << (16 * (j & 1));
+    }
     return v;
 }
 template <bool STREAM = false>
@@ -132,8 +143,11 @@ __device__ __forceinline__ void store8(uint16_t* row, int64_t c, int64_t cols, c
         else *p = v;
         return;
     }
-    for (int j = 0; j < 8; ++j)
-        if (c + j < cols) row[c + j] = (uint16_t)(v[j >> 1] >> (16 * (j & 1)));
+    const int n = (int)(cols - c);
+    if (n & 4) *reinterpret_cast<u32x2_anywhere*>(row + c) = u32x2{v[0], v[1]};
+    const uint32_t third = n & 4 ? v[2] : v[0], fourth = n & 4 ? v[3] : v[1];
+    if (n & 2) *reinterpret_cast<u32_anywhere*>(row + c + (n & 4)) = third;
+    if (n & 1) row[c + n - 1] = (uint16_t)(n & 2 ? fourth : third);
 }
 // Nearest BF16 value, ties to even; a NaN becomes the quiet NaN of its sign.
 __device__ __forceinline__ uint32_t bf16_of(float v) {

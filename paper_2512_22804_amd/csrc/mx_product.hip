@@ -381,7 +381,7 @@ __device__ __forceinline__ void multiply_step(f32x16 (&acc)[S::FM][S::FN], const
 // accumulators hold 4 columns of 32 rows.  `kCols` columns at a time; pieces lie permuted by the row against bank conflicts.
 template <bool F32, int FM, int FN, int BYTES, int AUX>
 __device__ __forceinline__ void store_tile(const MxProductArgs& p, uint8_t* lds, f32x16 (&acc)[FM][FN], int64_t base, int64_t m0, int64_t m_end,
-                                           int64_t n0, int lane, bool whole) {
+                                           int64_t n0, int lane, bool words) {
     constexpr int kSize = F32 ? 4 : 2;
     constexpr int kMost = BYTES / (FM * 32) >= 256 ? 256 : 128;                 // bytes of a row at a time
     constexpr int kCols = FN * 32 * kSize > kMost ? kMost / kSize : FN * 32;
@@ -403,27 +403,30 @@ __device__ __forceinline__ void store_tile(const MxProductArgs& p, uint8_t* lds,
                 }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         const int piece = lane % kPieces, first = lane / kPieces;
-        if (whole) {
-            // whole rows of 4-byte words: rows from `m_end` on lie outside the buffer; always the same number of stores
-            const int64_t rows = min(m_end - m0, (int64_t)FM * 32);
+        const int64_t n = n0 + c0 + piece * (16 / kSize);
+        const bool inside = n + 16 / kSize <= p.n;      // a whole piece
+        if (words) {
+            // Rows of 4-byte words: those from `m_end` on and pieces that are not whole lie outside the buffer, which ends with the last
+            // row's last column; always the same number of stores.
+            const int64_t rows = min(m_end - m0, (int64_t)FM * 32), columns = min((int64_t)kCols, max(p.n - n0 - c0, (int64_t)0));
             const uint32_t ld = (uint32_t)p.ldc * kSize;
             const BufRsrc out = make_buf_window(reinterpret_cast<uint8_t*>(p.c) + (base + m0 * p.ldc + n0 + c0) * kSize,
-                                                rows > 0 ? (uint32_t)(rows - 1) * ld + kRow : 0u);
-            uint32_t at = first * ld + piece * 16;
+                                                rows > 0 ? (uint32_t)(rows - 1) * ld + (uint32_t)columns * kSize : 0u);
+            uint32_t at = inside ? first * ld + piece * 16 : kNowhere;              // (which 128 rows more do not bring back into range)
 #pragma unroll
             for (int r = 0; r < FM * 32; r += kLanes) {
                 const int row_r = first + r;            // its swizzle repeats: kLanes divides kPieces or the other way round
                 buf_store16<AUX>(out, at, *reinterpret_cast<const u32x4*>(lds + row_r * kRow + (piece ^ (row_r & (kPieces - 1))) * 16));
                 at += kLanes * ld;
             }
-        } else {
-            const int64_t n = n0 + c0 + piece * (16 / kSize);
+        }
+        if (n < p.n && !(words && inside)) {
 #pragma unroll 1
             for (int r = first; r < FM * 32; r += kLanes) {
-                if (m0 + r >= m_end || n >= p.n) break;
+                if (m0 + r >= m_end) break;
                 const uint8_t* v = lds + r * kRow + (piece ^ (r & (kPieces - 1))) * 16;
                 uint8_t* c = reinterpret_cast<uint8_t*>(p.c) + (base + (m0 + r) * p.ldc + n) * kSize;
-                if (n + 16 / kSize <= p.n) __builtin_memcpy(c, v, 16);
+                if (inside) __builtin_memcpy(c, v, 16);
                 else {
 #pragma unroll 1
                     for (int e = 0; n + e < p.n; ++e) __builtin_memcpy(c + e * kSize, v + e * kSize, kSize);    // the last columns
@@ -595,7 +598,7 @@ __device__ __forceinline__ void take_tiles(const MxProductArgs& p, Walk& walk, u
     request_scales<S>(lds_at + S::kScalesAt, w.q, 0, wave);
 #pragma unroll
     for (int i = 0; i < S::kRequests; ++i) request_codes<S>(lds_at, w.q, 0, wave, i);
-    bool stored = false;                                // whole rows were, kStores of them behind the first stage's requests
+    bool stored = false;                                // kStores stores at least were issued behind the first stage's requests
     for (;;) {
 #pragma unroll
         for (int i = 0; i < S::kFirstRequests; ++i) request_codes<S>(lds_at + S::kCodes, w.q, 1, wave, i);
@@ -655,7 +658,7 @@ __device__ __forceinline__ void take_tiles(const MxProductArgs& p, Walk& walk, u
             for (int i = 0; i < S::kRequests; ++i) request_codes<S>(lds_at, w.q, 0, wave, i);
         }
         settle(acc);
-        stored = p.c_words && n0 + FN * 32 <= p.n;
+        stored = p.c_words;
         int own_lane = lane;                            // (as if new for every tile: its addresses are not kept in registers all along)
         asm volatile("" : "+v"(own_lane));
         store_tile<F32, FM, FN, S::kCodes / 4, MODE == kMxDepth ? kBufStoreAux : 0>(p, lds + S::kCodes + wave * (S::kCodes / 4), acc, base, m0, m_end, n0, own_lane, stored);
