@@ -61,6 +61,7 @@ struct MxProductArgs {
     int32_t  f32;                       // C in binary32, else BF16
     int32_t  splits;                    // (launcher) kMxDense: parts of the depth, each with a C of its own, batch_c apart
     int32_t  c_words;                   // (launcher) rows of C are whole 4-byte words and near each other
+    int32_t  c_lines;                   // and of whole lines of 128 bytes
 };
 size_t mx_product_workspace(int64_t m, int64_t n, int64_t blocks);
 hipError_t launch_mx_product(int mode, MxProductArgs p, void* workspace, hipStream_t st);

@@ -1,6 +1,7 @@
 // Products of microscaled 4-bit operands on the matrix cores.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "mx_device.h"
 #include "mx_launch.h"
@@ -379,7 +380,7 @@ __device__ __forceinline__ void multiply_step(f32x16 (&acc)[S::FM][S::FN], const
 
 // A wave's sums to C by way of its LDS buffer, so that every row is written in pieces of 16 neighbouring bytes per lane: the
 // accumulators hold 4 columns of 32 rows.  `kCols` columns at a time; pieces lie permuted by the row against bank conflicts.
-template <bool F32, int FM, int FN, int BYTES, int AUX>
+template <bool F32, int FM, int FN, int BYTES, bool DEPTH>
 __device__ __forceinline__ void store_tile(const MxProductArgs& p, uint8_t* lds, f32x16 (&acc)[FM][FN], int64_t base, int64_t m0, int64_t m_end,
                                            int64_t n0, int lane, bool words) {
     constexpr int kSize = F32 ? 4 : 2;
@@ -412,13 +413,20 @@ __device__ __forceinline__ void store_tile(const MxProductArgs& p, uint8_t* lds,
             const uint32_t ld = (uint32_t)p.ldc * kSize;
             const BufRsrc out = make_buf_window(reinterpret_cast<uint8_t*>(p.c) + (base + m0 * p.ldc + n0 + c0) * kSize,
                                                 rows > 0 ? (uint32_t)(rows - 1) * ld + (uint32_t)columns * kSize : 0u);
-            uint32_t at = inside ? first * ld + piece * 16 : kNowhere;              // (which 128 rows more do not bring back into range)
+            const uint32_t start = inside ? first * ld + piece * 16 : kNowhere;     // (which 128 rows more do not bring back into range)
+            const auto store_rows = [&](auto aux) {
+                uint32_t at = start;
 #pragma unroll
-            for (int r = 0; r < FM * 32; r += kLanes) {
-                const int row_r = first + r;            // its swizzle repeats: kLanes divides kPieces or the other way round
-                buf_store16<AUX>(out, at, *reinterpret_cast<const u32x4*>(lds + row_r * kRow + (piece ^ (row_r & (kPieces - 1))) * 16));
-                at += kLanes * ld;
-            }
+                for (int r = 0; r < FM * 32; r += kLanes) {
+                    const int row_r = first + r;        // its swizzle repeats: kLanes divides kPieces or the other way round
+                    buf_store16<decltype(aux)::value>(out, at, *reinterpret_cast<const u32x4*>(lds + row_r * kRow + (piece ^ (row_r & (kPieces - 1))) * 16));
+                    at += kLanes * ld;
+                }
+            };
+            // The experts' results, as large as their weights, go past the caches if their rows consist of whole lines (16 of 2048 x 4096:
+            // 147 us, 170 through the caches; 60 of 442 x 1000, whose lines two waves write: 42 and 29).
+            if (DEPTH && p.c_lines) store_rows(std::integral_constant<int, kBufStoreNt>{});
+            else store_rows(std::integral_constant<int, 0>{});
         }
         if (n < p.n && !(words && inside)) {
 #pragma unroll 1
@@ -661,7 +669,7 @@ __device__ __forceinline__ void take_tiles(const MxProductArgs& p, Walk& walk, u
         stored = p.c_words;
         int own_lane = lane;                            // (as if new for every tile: its addresses are not kept in registers all along)
         asm volatile("" : "+v"(own_lane));
-        store_tile<F32, FM, FN, S::kCodes / 4, MODE == kMxDepth ? kBufStoreAux : 0>(p, lds + S::kCodes + wave * (S::kCodes / 4), acc, base, m0, m_end, n0, own_lane, stored);
+        store_tile<F32, FM, FN, S::kCodes / 4, MODE == kMxDepth>(p, lds + S::kCodes + wave * (S::kCodes / 4), acc, base, m0, m_end, n0, own_lane, stored);
         if (!walk.left) break;
         __syncthreads();                                // every wave has read what it put into the second buffer
     }
@@ -874,6 +882,7 @@ static bool near_rows(const MxProductArgs& p) {         // 256 rows of either op
 static hipError_t launch_all_tiles(int mode, MxProductArgs p, bool large, hipStream_t st) {
     const int64_t size = p.f32 ? 4 : 2;
     p.c_words = ((reinterpret_cast<uintptr_t>(p.c) | (uintptr_t)(p.ldc * size) | (uintptr_t)(p.batch_c * size)) & 3) == 0 && 256 * p.ldc * size < 0x7FFFFFFFll;
+    p.c_lines = ((reinterpret_cast<uintptr_t>(p.c) | (uintptr_t)(p.ldc * size) | (uintptr_t)(p.batch_c * size)) & 127) == 0;
     if (large) return p.f32 ? launch_tiles<true, 256, 256, 1>(mode, p, st) : launch_tiles<false, 256, 256, 1>(mode, p, st);
     return p.f32 ? launch_tiles<true, 128, 128, 2>(mode, p, st) : launch_tiles<false, 128, 128, 2>(mode, p, st);
 }
