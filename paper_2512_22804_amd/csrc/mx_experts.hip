@@ -147,25 +147,29 @@ __device__ __forceinline__ u32x4 narrow8(const float (&f)[8]) {
     return v;
 }
 
-constexpr int kRowSpan = 1024;          // elements of a row that one wave moves: two chunks per lane
+// Elements of a row that one wave moves: two chunks per lane.  The spans of a row follow each other, not the rows of a span (sums of two
+// rows of 4096 for each of 8192 tokens: 33 us, 42 the other way).
+constexpr int kRowSpan = 1024;
 
 template <bool STREAM>
-__global__ __launch_bounds__(256) void k_expert_gather(const uint16_t* x, int64_t ld_x, int64_t d, MxOrder o, uint16_t* xs, int64_t ld_xs) {
-    const int64_t slot = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+__global__ __launch_bounds__(256) void k_expert_gather(const uint16_t* x, int64_t ld_x, int64_t d, MxOrder o, uint16_t* xs, int64_t ld_xs, uint32_t spans) {
+    const uint32_t group = blockIdx.x / spans, span = blockIdx.x - group * spans;
+    const int64_t slot = (int64_t)group * 4 + (threadIdx.x >> 6);
     if (slot >= o.capacity) return;
     const uint32_t choice = (uint32_t)o.src[slot], choices = (uint32_t)o.tokens * (uint32_t)o.top_k;
     const uint16_t* row = choice < choices ? x + (int64_t)(choice / (uint32_t)o.top_k) * ld_x : nullptr;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        const int64_t c = (int64_t)blockIdx.y * kRowSpan + h * 512 + (threadIdx.x & 63) * 8;
+        const int64_t c = (int64_t)span * kRowSpan + h * 512 + (threadIdx.x & 63) * 8;
         if (c < d) store8<STREAM>(xs + slot * ld_xs, c, d, row ? load8(row, c, d) : u32x4{0u, 0u, 0u, 0u});
     }
 }
 
 template <bool WEIGHTS, bool STREAM>
 __global__ __launch_bounds__(256) void k_expert_combine(const uint16_t* ys, int64_t ld_ys, int64_t d, MxOrder o, const float* weights,
-                                                        uint16_t* y, int64_t ld_y) {
-    const int64_t token = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+                                                        uint16_t* y, int64_t ld_y, uint32_t spans) {
+    const uint32_t group = blockIdx.x / spans, span = blockIdx.x - group * spans;
+    const int64_t token = (int64_t)group * 4 + (threadIdx.x >> 6);
     if (token >= o.tokens) return;
     float acc[2][8] = {};
     // the rows of up to four choices are on their way at once; they are added in order
@@ -184,7 +188,7 @@ __global__ __launch_bounds__(256) void k_expert_combine(const uint16_t* ys, int6
         for (int j = 0; j < kAtOnce; ++j)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int64_t c = (int64_t)blockIdx.y * kRowSpan + h * 512 + (threadIdx.x & 63) * 8;
+                const int64_t c = (int64_t)span * kRowSpan + h * 512 + (threadIdx.x & 63) * 8;
                 rows[j][h] = slot[j] < (uint32_t)o.capacity && c < d ? load8<STREAM>(ys + slot[j] * ld_ys, c, d) : u32x4{0u, 0u, 0u, 0u};
             }
 #pragma unroll
@@ -201,7 +205,7 @@ __global__ __launch_bounds__(256) void k_expert_combine(const uint16_t* ys, int6
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        const int64_t c = (int64_t)blockIdx.y * kRowSpan + h * 512 + (threadIdx.x & 63) * 8;
+        const int64_t c = (int64_t)span * kRowSpan + h * 512 + (threadIdx.x & 63) * 8;
         if (c < d) store8<STREAM>(y + token * ld_y, c, d, narrow8(acc[h]));
     }
 }
@@ -246,7 +250,6 @@ __global__ __launch_bounds__(256) void k_expert_combine_backward(const uint16_t*
 }
 
 uint32_t four_per_block(int64_t n) { return (uint32_t)((n + 3) / 4); }
-bool streamed(const MxOrder& o, int64_t d) { return (int64_t)o.capacity * d * 2 >= kMxStreamBytes; }
 uint32_t row_spans(int64_t d) { return (uint32_t)((d + kRowSpan - 1) / kRowSpan); }
 
 }  // namespace
@@ -280,21 +283,28 @@ hipError_t launch_expert_sort(const int32_t* ids, const MxOrder& o, void* worksp
 }
 
 hipError_t launch_expert_gather(const uint16_t* x, int64_t ld_x, int64_t d, const MxOrder& o, uint16_t* xs, int64_t ld_xs, hipStream_t st) {
-    const dim3 grid(four_per_block(o.capacity), row_spans(d));
-    if (streamed(o, d)) k_expert_gather<true><<<grid, dim3(256), 0, st>>>(x, ld_x, d, o, xs, ld_xs);
-    else k_expert_gather<false><<<grid, dim3(256), 0, st>>>(x, ld_x, d, o, xs, ld_xs);
+    const uint32_t spans = row_spans(d);
+    const int64_t blocks = (int64_t)four_per_block(o.capacity) * spans;
+    if (blocks > 0x7FFFFFFFll) return hipErrorInvalidValue;
+    const dim3 grid((uint32_t)blocks);
+    if (mx_streamed(o.capacity * d, xs, ld_xs, 0)) k_expert_gather<true><<<grid, dim3(256), 0, st>>>(x, ld_x, d, o, xs, ld_xs, spans);
+    else k_expert_gather<false><<<grid, dim3(256), 0, st>>>(x, ld_x, d, o, xs, ld_xs, spans);
     return hipGetLastError();
 }
 
 hipError_t launch_expert_combine(const uint16_t* ys, int64_t ld_ys, int64_t d, const MxOrder& o, const float* weights, uint16_t* y,
                                  int64_t ld_y, hipStream_t st) {
-    const dim3 grid(four_per_block(o.tokens), row_spans(d));
+    const uint32_t spans = row_spans(d);
+    const int64_t blocks = (int64_t)four_per_block(o.tokens) * spans;
+    if (blocks > 0x7FFFFFFFll) return hipErrorInvalidValue;
+    const dim3 grid((uint32_t)blocks);
+    const bool stream = mx_streamed(o.capacity * d, ys, ld_ys, 0) && mx_streamed(o.capacity * d, y, ld_y, 0);
     if (weights) {
-        if (streamed(o, d)) k_expert_combine<true, true><<<grid, dim3(256), 0, st>>>(ys, ld_ys, d, o, weights, y, ld_y);
-        else k_expert_combine<true, false><<<grid, dim3(256), 0, st>>>(ys, ld_ys, d, o, weights, y, ld_y);
+        if (stream) k_expert_combine<true, true><<<grid, dim3(256), 0, st>>>(ys, ld_ys, d, o, weights, y, ld_y, spans);
+        else k_expert_combine<true, false><<<grid, dim3(256), 0, st>>>(ys, ld_ys, d, o, weights, y, ld_y, spans);
     } else {
-        if (streamed(o, d)) k_expert_combine<false, true><<<grid, dim3(256), 0, st>>>(ys, ld_ys, d, o, weights, y, ld_y);
-        else k_expert_combine<false, false><<<grid, dim3(256), 0, st>>>(ys, ld_ys, d, o, weights, y, ld_y);
+        if (stream) k_expert_combine<false, true><<<grid, dim3(256), 0, st>>>(ys, ld_ys, d, o, weights, y, ld_y, spans);
+        else k_expert_combine<false, false><<<grid, dim3(256), 0, st>>>(ys, ld_ys, d, o, weights, y, ld_y, spans);
     }
     return hipGetLastError();
 }
@@ -309,7 +319,7 @@ static void combine_backward(const uint16_t* dy, int64_t ld_dy, const uint16_t* 
 }
 hipError_t launch_expert_combine_backward(const uint16_t* dy, int64_t ld_dy, const uint16_t* ys, int64_t ld_ys, int64_t d, const MxOrder& o,
                                           const float* weights, uint16_t* dys, int64_t ld_dys, float* dweights, hipStream_t st) {
-    if (streamed(o, d)) combine_backward<true>(dy, ld_dy, ys, ld_ys, d, o, weights, dys, ld_dys, dweights, st);
+    if ((!ys || mx_streamed(o.capacity * d, ys, ld_ys, 0)) && (!dys || mx_streamed(o.capacity * d, dys, ld_dys, 0))) combine_backward<true>(dy, ld_dy, ys, ld_ys, d, o, weights, dys, ld_dys, dweights, st);
     else combine_backward<false>(dy, ld_dy, ys, ld_ys, d, o, weights, dys, ld_dys, dweights, st);
     return hipGetLastError();
 }

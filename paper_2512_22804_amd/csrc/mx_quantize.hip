@@ -19,8 +19,8 @@ __global__ __launch_bounds__(256, T && WEIGHTED ? 3 : 1) void k_mx_quantize(MxQu
     __shared__ __align__(16) uint32_t tile[T ? 128 * 64 : 4];
     __shared__ __align__(16) float row_weight[WEIGHTED ? RPT * 16 : 1];
     const int t = threadIdx.x;
-    const uint32_t ct = blockIdx.x % col_tiles;
-    const int64_t rt = blockIdx.x / col_tiles;
+    const uint32_t tile_id = tile_of(blockIdx.x, gridDim.x), ct = tile_id % col_tiles;
+    const int64_t rt = tile_id / col_tiles;
     const int64_t c0 = (int64_t)ct * kTileCols, r0 = rt * (RPT * 16);
     const uint32_t z = blockIdx.z;
     const uint16_t* x = a.x + (int64_t)z * a.batch_x;
@@ -170,9 +170,9 @@ __global__ __launch_bounds__(256) void k_mx_quantize_tokens(MxQuantArgs a, uint3
         }
         return;
     }
-    const uint32_t ct = blockIdx.x % col_tiles;
+    const uint32_t tile_id = tile_of(blockIdx.x, token_groups), ct = tile_id % col_tiles;
     const int64_t c = (int64_t)ct * kTileCols + (t & 15) * 8, block = c / kMxBlock;
-    const int64_t token0 = (int64_t)(blockIdx.x / col_tiles) * (RPT * 16) + (t >> 4);
+    const int64_t token0 = (int64_t)(tile_id / col_tiles) * (RPT * 16) + (t >> 4);
     const uint32_t tokens = a.choices / a.top_k;
     constexpr uint32_t kAtOnce = 2;                     // slots on their way with the rows
     u32x4 v[RPT];
@@ -211,9 +211,9 @@ __global__ __launch_bounds__(256) void k_mx_quantize_tokens(MxQuantArgs a, uint3
 template <int RPT, bool STREAM>
 __global__ __launch_bounds__(256) void k_mx_dequantize(int64_t rows, int64_t cols, MxOperand op, uint16_t* y, int64_t ld_y, int64_t batch_y,
                                                        uint32_t col_tiles) {
-    const uint32_t ct = blockIdx.x % col_tiles;
+    const uint32_t tile_id = tile_of(blockIdx.x, gridDim.x), ct = tile_id % col_tiles;
     const int64_t c = (int64_t)ct * kTileCols + (threadIdx.x & 15) * 8;
-    const int64_t r0 = (int64_t)(blockIdx.x / col_tiles) * (16 * RPT) + (threadIdx.x >> 4);
+    const int64_t r0 = (int64_t)(tile_id / col_tiles) * (16 * RPT) + (threadIdx.x >> 4);
     const uint32_t z = blockIdx.z;
     if (c >= cols) return;
     uint32_t codes[RPT], byte[RPT];
@@ -268,7 +268,7 @@ hipError_t launch_mx_quantize(const MxQuantArgs& a, hipStream_t st) {
     if (tiles > 0x7FFFFFFFll) return hipErrorInvalidValue;
     const dim3 grid((uint32_t)tiles, 1, (uint32_t)a.batch);
     // rows gathered by expert are read several times; the rows form alone is no faster past the caches (19.1 us against 19.7)
-    const bool stream = t_form && a.src == nullptr && a.rows * a.cols * a.batch * 2 >= kMxStreamBytes;
+    const bool stream = t_form && a.src == nullptr && mx_streamed(a.rows * a.cols * a.batch, a.x, a.ld, a.batch_x);
     if (!t_form && tall) quantize_form<2, true, false, false>(a, col_tiles, grid, st);
     else if (!t_form) quantize_form<1, true, false, false>(a, col_tiles, grid, st);
     else if (rows_form && stream) quantize_form<8, true, true, true>(a, col_tiles, grid, st);
@@ -286,7 +286,7 @@ hipError_t launch_mx_dequantize(int64_t rows, int64_t cols, int64_t batch, const
     const int64_t tiles = ((rows + tile_rows - 1) / tile_rows) * col_tiles;
     if (tiles > 0x7FFFFFFFll) return hipErrorInvalidValue;
     const dim3 grid((uint32_t)tiles, 1, (uint32_t)batch);
-    if (rows * cols * batch * 2 >= kMxStreamBytes) k_mx_dequantize<2, true><<<grid, dim3(256), 0, st>>>(rows, cols, op, y, ld_y, batch_y, col_tiles);
+    if (mx_streamed(rows * cols * batch, y, ld_y, batch_y)) k_mx_dequantize<2, true><<<grid, dim3(256), 0, st>>>(rows, cols, op, y, ld_y, batch_y, col_tiles);
     else if (tall) k_mx_dequantize<2, false><<<grid, dim3(256), 0, st>>>(rows, cols, op, y, ld_y, batch_y, col_tiles);
     else k_mx_dequantize<1, false><<<grid, dim3(256), 0, st>>>(rows, cols, op, y, ld_y, batch_y, col_tiles);
     return hipGetLastError();
