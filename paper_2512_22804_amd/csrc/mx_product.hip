@@ -134,7 +134,7 @@ __device__ __forceinline__ void store4(const MxProductArgs& p, int64_t at, int64
 }
 
 // One wave: 32 rows of C x 64 columns, operands from global memory straight into registers.  For operands whose rows are too far
-// apart for the kernels below.
+// apart for the kernels below (2^31 bytes and more between 256 of them).
 constexpr int kWaveM = 32, kWaveN = 64;
 template <int MODE>
 __global__ __launch_bounds__(64) void k_mx_product(MxProductArgs p, uint32_t n_tiles) {
@@ -203,6 +203,11 @@ __global__ __launch_bounds__(64) void k_mx_product(MxProductArgs p, uint32_t n_t
 // lie outside the buffer resource's range and arrive as zeros; so do the pieces behind a row's last block, whose lanes request an
 // address out of range in the last stage, and stages beyond the last, whose range is empty.  The scale bytes behind the last
 // block, loaded 16 at a time, are replaced by 2^0: whatever they hold, a NaN too, counts for nothing.
+//
+// 8192 x 14336 x 4096: 241 us, 4.0 PFLOP/s.  The same instructions on random operands that stay in registers reach 6.6 at 1.7 GHz, the
+// clock that the power allows, and 9.6 on zeros; without the requests the loop would take a seventh less, and a tile's way out
+// (its sums through LDS to memory, at about 8 us of 35) is not covered by the next one's products, since the sums and
+// their successors do not both fit into the registers.
 
 constexpr uint32_t kNowhere = 0x7FFFFFFFu;              // an offset that no range contains
 
@@ -708,6 +713,8 @@ __global__ __launch_bounds__(256, GROUPS) void k_mx_tile(MxProductArgs p, uint32
 // Up to 64 rows of A (tokens) against all of B (weights): what counts is how fast B's bytes come in.  Eight waves share a
 // workgroup's 16 NT rows of B and split the depth between them, in groups of 512 (four matrix instructions); every wave has a
 // group's loads on their way at once, straight into registers.  The partial sums are joined through LDS, in the order of the waves.
+// (1 x 14336 x 4096: 8.0 us, 16 rows 9.9, 64 rows 14.5; B's bytes alone take 6.0 at the rate of a large copy.  The next group's loads
+// ahead of the products take twice the registers and so half of the waves: 10.4 us.)
 constexpr int kFewWaves = 8;
 template <int MODE, int MT, int NT>
 __global__ __launch_bounds__(kFewWaves * 64) void k_mx_few(MxProductArgs p, uint32_t n_tiles) {
