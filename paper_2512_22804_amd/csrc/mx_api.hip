@@ -224,8 +224,8 @@ mor_status mor_expert_combine_backward(const uint16_t* dy, int64_t ld_dy, const 
     mor_status st = check_order(order);
     if (st != MOR_OK) return st;
     if (d < 1 || d > kMaxDim) return MOR_ERR_SHAPE;
+    if (order->capacity == 0) return MOR_OK;            // empty gradients have no address
     if (!dys && !dweights) return MOR_ERR_NULL;
-    if (order->capacity == 0) return MOR_OK;
     if (order->tokens > 0) {
         if ((st = check_matrix(dy, ld_dy, d)) != MOR_OK) return st;
         if (dweights && (st = check_matrix(ys, ld_ys, d)) != MOR_OK) return st;

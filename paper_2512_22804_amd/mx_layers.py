@@ -26,6 +26,8 @@ def _check(x: torch.Tensor, w: torch.Tensor, dims: int) -> None:
 
 
 def _product(a: mx.MxOperand, b: mx.MxOperand, dtype: torch.dtype) -> torch.Tensor:
+    if a.cols == 0:                     # no tokens: a gradient without terms
+        return torch.zeros(a.rows, b.rows, dtype=dtype, device=a.codes.device)
     c = torch.empty(a.rows, b.rows, dtype=dtype, device=a.codes.device)
     mx.mor_mx_product(a, b, c, mx.alloc_product_workspace(a, b, c.device))
     return c

@@ -222,3 +222,64 @@ def test_wrong_inputs_raise():
         mx_layers.ServedExperts(w)(x[:, :32], ids, weights)
     with pytest.raises(binding.MorError):
         mx.mor_mx_quantize(x[:1].expand(4, 64), mx.alloc_operand(4, 64, DEV))       # rows upon each other
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_no_tokens(dtype):
+    w = made(40, 64, seed=2).to(DEV, dtype).requires_grad_()
+    x = torch.empty(0, 64, device=DEV, dtype=dtype).requires_grad_()
+    y = mx_layers.linear(x, w)
+    y.backward(torch.empty_like(y))
+    assert y.shape == (0, 40) and x.grad.shape == (0, 64) and (w.grad == 0).all()
+    w = made(3, 40, 64, seed=2).to(DEV, dtype).requires_grad_()
+    ids, weights = torch.empty(0, 2, device=DEV, dtype=torch.int32), torch.empty(0, 2, device=DEV).requires_grad_()
+    y = mx_layers.experts(x, w, ids, weights)
+    y.backward(torch.empty_like(y))
+    assert y.shape == (0, 40) and (w.grad == 0).all() and weights.grad.shape == (0, 2)
+    assert mx_layers.ServedExperts(w)(x, ids, weights.detach()).shape == (0, 40)
+
+
+@pytest.mark.gpu
+def test_every_choice_dropped():
+    x, w, ids, weights, dy = layer(5, 2, 3, 64, 40)
+    x, w = x.to(DEV).requires_grad_(), w.to(DEV).requires_grad_()
+    weights = torch.from_numpy(weights).to(DEV).requires_grad_()
+    y = mx_layers.experts(x, w, torch.full((5, 2), -1, device=DEV, dtype=torch.int32), weights)
+    y.backward(dy.to(DEV))
+    for t in (y, x.grad, w.grad, weights.grad):
+        assert (t == 0).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("which", [0, 1, 2])
+def test_experts_of_one_gradient(which):
+    x, w, ids, weights, dy = layer(50, 2, 4, 96, 72, seed=60)
+    ids, dy = torch.from_numpy(ids).to(DEV), dy.to(DEV)
+    every = [t.to(DEV).requires_grad_() for t in (x, w, torch.from_numpy(weights))]
+    mx_layers.experts(every[0], every[1], ids, every[2], seed=4).backward(dy)
+    one = [t.detach().clone().requires_grad_(i == which) for i, t in enumerate(every)]
+    mx_layers.experts(one[0], one[1], ids, one[2], seed=4).backward(dy)
+    assert torch.equal(one[which].grad, every[which].grad)
+
+
+@pytest.mark.gpu
+def test_layers_in_a_graph():
+    """Captured once, replayed on other inputs, with eager work in between."""
+    x, w, ids, weights, _ = layer(70, 2, 6, 64, 130, seed=80)
+    served, x, ids, weights = mx_layers.ServedExperts(w.to(DEV)), x.to(DEV), torch.from_numpy(ids).to(DEV), torch.from_numpy(weights).to(DEV)
+    with torch.cuda.stream(torch.cuda.Stream()):
+        served(x, ids, weights)                                             # (allocations before the capture)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = served(x, ids, weights)
+    for step in range(4):
+        x.copy_(made(70, 64, seed=90 + step))
+        ids.copy_(torch.randint(-1, 6, (70, 2), generator=torch.Generator().manual_seed(step), dtype=torch.int32))
+        want = served(x, ids, weights)
+        torch.cuda.synchronize()
+        y.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want)
