@@ -116,6 +116,7 @@ class MxOperand:
         if self.codes.device != self.scales.device:
             raise ValueError("codes and scales must live on one device")
         lone = self.rows == 1
+        object.__setattr__(self, "batch", self.codes.shape[0] if self.codes.dim() == 3 else 1)
         object.__setattr__(self, "_struct", MorMxOperand(
             None, self.codes.shape[-1] if lone else self.codes.stride(-2), None, self.scales.shape[-1] if lone else self.scales.stride(-2),
             self.codes.stride(0) if self.codes.dim() == 3 else 0, self.scales.stride(0) if self.scales.dim() == 3 else 0))
@@ -123,10 +124,6 @@ class MxOperand:
     @property
     def blocks(self) -> int:
         return -(-self.cols // BLOCK)
-
-    @property
-    def batch(self) -> int:
-        return self.codes.shape[0] if self.codes.dim() == 3 else 1
 
     def struct(self) -> int:
         """Address of the operand's structure, valid as long as the operand."""
