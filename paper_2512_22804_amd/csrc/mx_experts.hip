@@ -195,15 +195,16 @@ __global__ __launch_bounds__(256) void k_expert_combine(const uint16_t* ys, int6
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int64_t c = (int64_t)span * kRowSpan + h * 512 + (threadIdx.x & 63) * 8;
-                rows[j][h] = slot[j] < (uint32_t)o.capacity && c < d ? load8<STREAM>(ys + slot[j] * ld_ys, c, d) : u32x4{0u, 0u, 0u, 0u};
+                rows[j][h] = slot[j] < (uint32_t)o.capacity && c < d ? load8_start<STREAM>(ys + slot[j] * ld_ys, c, d) : u32x4{0u, 0u, 0u, 0u};
             }
 #pragma unroll
         for (int j = 0; j < kAtOnce; ++j) {
             if (slot[j] >= (uint32_t)o.capacity) continue;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
+                const int64_t c = (int64_t)span * kRowSpan + h * 512 + (threadIdx.x & 63) * 8;
                 float f[8];
-                widen8(rows[j][h], f);
+                widen8(c < d ? load8_end(rows[j][h], c, d) : rows[j][h], f);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) acc[h][i] += WEIGHTS ? w[j] * f[i] : f[i];
             }

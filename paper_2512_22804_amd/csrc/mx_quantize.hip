@@ -9,9 +9,10 @@ constexpr int64_t kManyElements = 1 << 22;  // from here on a lane takes several
 constexpr int kTileCols = 128;          // columns of a workgroup's tile: 16 lanes of 8 elements
 
 // One workgroup: RPT * 16 rows x 128 columns, 256 lanes.  Lane t holds 8 columns (16 bytes) of RPT rows; a block of the row
-// form is then 4 neighbouring lanes.  For the transposed form the tile goes through LDS (T: RPT = 8), and lane t takes a pair
-// of columns over 32 rows, so that a block's amax needs no other lane and its 16 bytes are one store; four neighbouring
-// lanes fill 64 bytes of an output row.  The rows of row block q are rotated by 16 q dwords: the four row blocks that
+// form is then 4 neighbouring lanes.  For the transposed form (T) the tile goes through LDS, and lane t takes a pair of columns over
+// 4 RPT rows.  RPT = 8: a block's 32 rows, so that its amax needs no other lane and its 16 bytes are one store; four neighbouring
+// lanes fill 64 bytes of an output row.  RPT = 2, for tensors of few tiles: 8 rows, four neighbouring lanes share a block, and a
+// lane's chain of work is a quarter as long.  The rows are rotated by 16 dwords every 4 RPT of them: those that
 // neighbouring lanes read then lie in different banks.
 //
 // Rounding to nearest is bound by memory (14336 x 4096: rows 31 us, transposed 32, both from one read 41 us = 4.3 TB/s), stochastic rounding
@@ -21,8 +22,9 @@ constexpr int kTileCols = 128;          // columns of a workgroup's tile: 16 lan
 // forms, stochastic: 54 us).
 template <int RPT, bool ROWS, bool T, bool SR, bool WEIGHTED, bool STREAM>
 __global__ __launch_bounds__(256, T && WEIGHTED ? 3 : 1) void k_mx_quantize(MxQuantArgs a, uint32_t col_tiles) {
-    static_assert(!T || RPT == 8, "the transposed form works on 128 x 128 tiles");
-    __shared__ __align__(16) uint32_t tile[T ? 128 * 64 : 4];
+    static_assert(!T || RPT == 8 || RPT == 2, "the transposed form works on tiles of 128 or 32 rows");
+    constexpr int kRows = T ? 4 * RPT : 8;              // of a lane in the transposed form
+    __shared__ __align__(16) uint32_t tile[T ? RPT * 16 * 64 : 4];
     __shared__ __align__(16) float row_weight[WEIGHTED ? RPT * 16 : 1];
     const int t = threadIdx.x;
     const uint32_t tile_id = tile_of(blockIdx.x, gridDim.x), ct = tile_id % col_tiles;
@@ -50,14 +52,17 @@ __global__ __launch_bounds__(256, T && WEIGHTED ? 3 : 1) void k_mx_quantize(MxQu
                 }
             }
         }
-        v[i] = row != nullptr && c < a.cols ? load8<STREAM>(row, c, a.cols) : u32x4{0u, 0u, 0u, 0u};
+        v[i] = row != nullptr && c < a.cols ? load8_start<STREAM>(row, c, a.cols) : u32x4{0u, 0u, 0u, 0u};
     }
+    if (c < a.cols)
+#pragma unroll
+        for (int i = 0; i < RPT; ++i) v[i] = load8_end(v[i], c, a.cols);
     const bool ceil_rule = a.ceil_rule != 0;
     if (T) {
 #pragma unroll
         for (int i = 0; i < RPT; ++i) {
             const int r = (t >> 4) + 16 * i;
-            *reinterpret_cast<u32x4*>(&tile[r * 64 + (((t & 15) * 4 + 16 * (r >> 5)) & 63)]) = v[i];
+            *reinterpret_cast<u32x4*>(&tile[r * 64 + (((t & 15) * 4 + 16 * (r / kRows)) & 63)]) = v[i];
             if (WEIGHTED && (t & 15) == 0) row_weight[r] = w[i];
         }
     }
@@ -100,38 +105,42 @@ __global__ __launch_bounds__(256, T && WEIGHTED ? 3 : 1) void k_mx_quantize(MxQu
     if (T) {
         const MxOperand o = a.out_t;
         __syncthreads();
-        const int q = t & 3, pair = t >> 2;
-        const int64_t col = c0 + 2 * pair, row0 = r0 + 32 * q;
-        uint32_t d[32];
+        const int q = t & 3, pair = t >> 2;             // the lane's rows begin with q kRows
+        const int64_t col = c0 + 2 * pair, row0 = r0 + q * kRows, block0 = row0 & ~31ll;
+        uint32_t d[kRows];
 #pragma unroll
-        for (int j = 0; j < 32; ++j) d[j] = tile[(32 * q + j) * 64 + ((pair + 16 * q) & 63)];
+        for (int j = 0; j < kRows; ++j) d[j] = tile[(kRows * q + j) * 64 + ((pair + 16 * q) & 63)];
         uint32_t m = 0u;
-        float w32[WEIGHTED ? 32 : 1];
+        float w_row[WEIGHTED ? kRows : 1];
         if (WEIGHTED) {
 #pragma unroll
-            for (int j = 0; j < 32; ++j) w32[j] = row_weight[32 * q + j];
+            for (int j = 0; j < kRows; ++j) w_row[j] = row_weight[kRows * q + j];
         } else {
 #pragma unroll
-            for (int j = 0; j < 32; ++j) m = pk_max_u16(m, d[j] & 0x7FFF7FFFu);
+            for (int j = 0; j < kRows; ++j) m = pk_max_u16(m, d[j] & 0x7FFF7FFFu);
         }
 #pragma unroll
         for (int side = 0; side < 2; ++side) {
-            float f[32];
+            float f[kRows];
             uint32_t amax = side ? m & 0xFFFF0000u : m << 16;
             if (SR || WEIGHTED) {
 #pragma unroll
-                for (int j = 0; j < 32; ++j) {
+                for (int j = 0; j < kRows; ++j) {
                     f[j] = __uint_as_float(side ? (d[j] & 0xFFFF0000u) : (d[j] << 16));
                     if (WEIGHTED) {
-                        f[j] *= w32[j];
+                        f[j] *= w_row[j];
                         amax = max(amax, __float_as_uint(f[j]) & 0x7FFFFFFFu);
                     }
                 }
             }
+            if (kRows == 8) {
+                amax = max(amax, (uint32_t)__shfl_xor((int)amax, 1));
+                amax = max(amax, (uint32_t)__shfl_xor((int)amax, 2));
+            }
             const uint32_t byte = mx_scale_byte(amax, ceil_rule);
-            u32x4 codes;
+            uint32_t codes[kRows / 8];
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
+            for (int g = 0; g < kRows / 8; ++g) {
                 if (SR || WEIGHTED) {
                     float f8[8];
 #pragma unroll
@@ -146,9 +155,11 @@ __global__ __launch_bounds__(256, T && WEIGHTED ? 3 : 1) void k_mx_quantize(MxQu
                     codes[g] = mx_codes8_nearest(p, byte);
                 }
             }
-            if (col + side < a.cols && row0 < a.rows) {
-                *reinterpret_cast<u32x4*>(o.codes + z * o.batch + (col + side) * o.ld + (row0 >> 1)) = codes;
-                o.scales[z * o.batch_s + (col + side) * o.ld_s + (row0 >> 5)] = (uint8_t)byte;
+            if (col + side < a.cols && block0 < a.rows) {
+                uint8_t* at = o.codes + z * o.batch + (col + side) * o.ld + (row0 >> 1);
+                if constexpr (kRows == 32) *reinterpret_cast<u32x4*>(at) = u32x4{codes[0], codes[1], codes[2], codes[3]};
+                else *reinterpret_cast<uint32_t*>(at) = codes[0];
+                if (row0 == block0) o.scales[z * o.batch_s + (col + side) * o.ld_s + (block0 >> 5)] = (uint8_t)byte;
             }
         }
     }
@@ -187,7 +198,7 @@ __global__ __launch_bounds__(256) void k_mx_quantize_tokens(MxQuantArgs a, uint3
 #pragma unroll
     for (int i = 0; i < RPT; ++i) {
         const int64_t token = token0 + 16 * i;
-        v[i] = token < tokens && c < a.cols ? load8(a.x + token * a.ld, c, a.cols) : u32x4{0u, 0u, 0u, 0u};
+        v[i] = token < tokens && c < a.cols ? load8_start(a.x + token * a.ld, c, a.cols) : u32x4{0u, 0u, 0u, 0u};
 #pragma unroll
         for (uint32_t j = 0; j < kAtOnce; ++j)
             slots[i][j] = token < tokens && j < a.top_k ? (uint32_t)a.slot_of[token * a.top_k + j] : ~0u;
@@ -196,6 +207,7 @@ __global__ __launch_bounds__(256) void k_mx_quantize_tokens(MxQuantArgs a, uint3
     for (int i = 0; i < RPT; ++i) {
         const int64_t token = token0 + 16 * i;
         uint32_t m = 0u;
+        if (c < a.cols) v[i] = load8_end(v[i], c, a.cols);
 #pragma unroll
         for (int j = 0; j < 4; ++j) m = pk_max_u16(m, v[i][j] & 0x7FFF7FFFu);
         uint32_t amax = fold_max16(m) << 16;
@@ -263,7 +275,11 @@ hipError_t launch_mx_quantize(const MxQuantArgs& a, hipStream_t st) {
     const uint32_t col_tiles = (uint32_t)((a.cols + kTileCols - 1) / kTileCols);
     const bool rows_form = a.out.codes != nullptr, t_form = a.out_t.codes != nullptr;
     const bool tall = a.rows * a.cols > kManyElements;
-    const int tile_rows = t_form ? 128 : tall ? 32 : 16;
+    // Tiles of 32 rows in the transposed form where those of 128 would be few, for which a lane's chain of work counts, not memory.  (Both
+    // forms, nearest and stochastic, with tiles of 32 and of 128 rows: 1024 x 1024 3.6, 4.4 and 5.7, 8.7 us; 2048 x 4096 9.4, 13.1 and
+    // 9.7, 14.9; 6144 x 4096 24.7, 31.9 and 22.0, 32.5; 14336 x 4096 58, 68 and 42, 62.)
+    const bool short_t = t_form && (a.rows + 127) / 128 * col_tiles * a.batch <= (a.stochastic ? 1024 : 256);
+    const int tile_rows = t_form ? short_t ? 32 : 128 : tall ? 32 : 16;
     if (a.src && !t_form && !a.weights && !a.stochastic) {
         const int64_t groups = ((int64_t)(a.choices / a.top_k) + tile_rows - 1) / tile_rows * col_tiles, fill = (a.rows + kFillSlots - 1) / kFillSlots;
         if (groups + fill > 0x7FFFFFFFll) return hipErrorInvalidValue;
@@ -279,6 +295,8 @@ hipError_t launch_mx_quantize(const MxQuantArgs& a, hipStream_t st) {
     const bool stream = t_form && a.src == nullptr && mx_streamed(a.rows * a.cols * a.batch, a.x, a.ld, a.batch_x);
     if (!t_form && tall) quantize_form<2, true, false, false>(a, col_tiles, grid, st);
     else if (!t_form) quantize_form<1, true, false, false>(a, col_tiles, grid, st);
+    else if (short_t && rows_form) quantize_form<2, true, true, false>(a, col_tiles, grid, st);
+    else if (short_t) quantize_form<2, false, true, false>(a, col_tiles, grid, st);
     else if (rows_form && stream) quantize_form<8, true, true, true>(a, col_tiles, grid, st);
     else if (rows_form) quantize_form<8, true, true, false>(a, col_tiles, grid, st);
     else if (stream) quantize_form<8, false, true, true>(a, col_tiles, grid, st);

@@ -84,3 +84,31 @@ def test_few_rows_of_experts(tokens, top_k, experts, n, k):
     for e in range(experts):
         s = slice(starts[e], starts[e + 1])
         close(got[s], av[s], bv[e], True, k)
+
+
+# transposed forms in tiles of 128 rows and of 32, weighted or not, in batches; the last tile of rows and of columns short
+@pytest.mark.parametrize("rounding", ["nearest", "stochastic"])
+@pytest.mark.parametrize("batch, rows, cols", [(1, 4200, 1030), (1, 33, 33000), (3, 500, 700), (9, 500, 1003), (1, 8300, 2100), (1, 31, 5), (2, 1, 300)])
+def test_transposed_forms(batch, rows, cols, rounding):
+    rng = np.random.default_rng(rows)
+    bits = rng.integers(0, 2 ** 16, (batch, rows, cols)).astype(np.uint16)
+    bits[(bits & 0x7F80) == 0x7F80] = 0x3F80
+    values = (bits.astype(np.uint32) << 16).view(np.float32).astype(np.float64)
+    values = np.where(np.abs(values) < 2.0 ** -100, 0.0, values)
+    bits = np.where(values == 0.0, 0, bits).astype(np.uint16)
+    x = torch.from_numpy(bits.view(np.int16)).to(DEV)
+    out, out_t = mx.alloc_operand(rows, cols, DEV, batch=batch), mx.alloc_operand(cols, rows, DEV, batch=batch)
+    for t in (out.codes, out.scales, out_t.codes, out_t.scales):
+        t.fill_(0xA5)
+    mx.mor_mx_quantize(x, out, out_t, rounding=rounding, seed=77)
+    alone = mx.alloc_operand(cols, rows, DEV, batch=batch)
+    mx.mor_mx_quantize(x, None, alone, rounding=rounding, seed=77)
+    blocks = -(-rows // 32)
+    assert torch.equal(alone.codes, out_t.codes) and torch.equal(alone.scales[..., :blocks], out_t.scales[..., :blocks])
+    for z in range(0, batch, 4):
+        for op, v, form in ((out, values[z], 0), (out_t, values[z].T, 1)):
+            noise = R.random16(*v.shape, form, 77, z) if rounding == "stochastic" else None
+            codes, scales, _ = R.quantize(v, "floor", noise)
+            got = R.unpack_codes(op.codes[z].cpu().numpy(), op.codes.shape[-1] * 2)
+            assert np.array_equal(got[:, :v.shape[1]], codes) and (got[:, v.shape[1]:] == 0).all()
+            assert np.array_equal(op.scales[z].cpu().numpy()[:, :scales.shape[1]], scales)
