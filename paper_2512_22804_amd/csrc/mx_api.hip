@@ -151,6 +151,8 @@ mor_status mor_mx_product_rows(int64_t n, int64_t k, const mor_mx_operand* a, co
     p.batch_bs = batched ? b->batch_scales : 0;
     p.offsets = order->offsets;
     p.n_experts = order->n_experts;
+    p.choices = order->tokens * order->top_k;
+    p.align = order->align;
     return launched(mor::launch_mx_product(mor::kMxRows, p, nullptr, (hipStream_t)stream));
 }
 

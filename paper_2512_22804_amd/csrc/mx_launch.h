@@ -61,12 +61,13 @@ struct MxProductArgs {
     int32_t  blocks;                    // blocks of 32 along the depth
     const int32_t* offsets;             // experts' segments (kMxRows, kMxDepth)
     int32_t  n_experts;
+    int32_t  choices, align;            // of the order: how many tiles to expect (kMxRows)
     int32_t  f32;                       // C in binary32, else BF16
     int32_t  splits;                    // (launcher) kMxDense: parts of the depth, each with a C of its own, batch_c apart
     int32_t  c_words;                   // (launcher) rows of C are whole 4-byte words and near each other
     int32_t  c_lines;                   // and of whole lines of 128 bytes
 };
-size_t mx_product_workspace(int64_t m, int64_t n, int64_t blocks);
+size_t mx_product_workspace(int64_t m, int64_t n, int32_t blocks);
 hipError_t launch_mx_product(int mode, MxProductArgs p, void* workspace, hipStream_t st);
 
 size_t mx_sort_workspace(int64_t choices, int64_t n_experts);

@@ -710,7 +710,7 @@ __global__ __launch_bounds__(256, GROUPS) void k_mx_tile(MxProductArgs p, uint32
 
 // ---- few rows ---------------------------------------------------------------------------------------------------------
 //
-// Up to 64 rows of A (tokens) against all of B (weights): what counts is how fast B's bytes come in.  Eight waves share a
+// Few rows of A (tokens), up to 64 per workgroup, against all of B (weights): what counts is how fast B's bytes come in.  Eight waves share a
 // workgroup's 16 NT rows of B and split the depth between them, in groups of 512 (four matrix instructions); every wave has a
 // group's loads on their way at once, straight into registers.  The partial sums are joined through LDS, in the order of the waves.
 // (1 x 14336 x 4096: 8.0 us, 16 rows 9.9, 64 rows 14.5; B's bytes alone take 6.0 at the rate of a large copy.  The next group's loads
@@ -815,31 +815,54 @@ __global__ __launch_bounds__(256) void k_mx_join(MxProductArgs p, const float* p
 // Which kernel a product of a given size takes.  Times in us, measured on whole and partly filled cards: a stage of a 256 x 256 tile
 // 1.9, of two 128 x 128 tiles on a CU 1.29, of one 0.56, and what a tile costs besides 8 and 5.  (In large tiles and in small ones,
 // us: 4096 x 4096 x 4096 38 and 47, 4096 x 5120 x 512 16.8 and 17.4, 2048 x 4096 x 4096 30.1 and 27.6, 1024 x 4096 x 4096 27.9 and 17.1.)
-constexpr int64_t kFewNarrow = 160;      // workgroups of few rows that the CUs want at least
 struct ProductPlan {
     enum { kFew, kSmallTiles, kLargeTiles } kind;
     int splits;                         // parts of the depth
+    int mt, nt;                         // kFew: 16 rows of A and of B of a workgroup
 };
-static ProductPlan plan_product(int mode, int64_t m, int64_t n, int64_t blocks, int64_t experts) {
+// The more rows of B a workgroup takes, the less often A's are read (64 x 14336 x 4096: 30.5 us with 16, 18.6 with 32, 14.5 with 64), but
+// the CUs want 160 workgroups at least (64 x 4096 x 4096: 8.6, 10.0, 13.4).  `rows`: of B, times the workgroups for A's.
+static int few_nt(double rows) { return rows < 160 * 32 ? 1 : rows < 160 * 64 ? 2 : 4; }
+
+// Tiles of `height` rows: of a product, of all experts' results, or to expect in the segments of experts, which end in part tiles.
+static double tile_rows(int mode, const MxProductArgs& p, int height) {
+    if (mode != kMxRows) return (double)((p.m + height - 1) / height) * (mode == kMxDepth ? p.n_experts : 1);
+    const double used = std::max(std::min(p.n_experts, p.choices), 1);
+    const double each = std::max((double)p.choices / used + 0.5 * (p.align - 1), (double)p.align);      // rows with those that fill up
+    return std::min(used * std::max(each / height + (height > p.align ? 0.5 * (1.0 - (double)p.align / height) : 0.0), 1.0),
+                    (double)p.m / height + used);
+}
+
+static ProductPlan plan_product(int mode, const MxProductArgs& p) {
+    const int64_t m = p.m, n = p.n, blocks = p.blocks;
     // (More than 32 rows and a long depth for few workgroups: parts of the depth are better.  64 x 4096 x 14336: 22.5 us, 18.8 in tiles;
-    // 64 x 4096 x 8192: 15.3 and 17.3.)
-    if (mode == kMxDense && m <= 64 && !(m > 32 && n < kFewNarrow * 32 && blocks > 320)) return {ProductPlan::kFew, 1};
+    // 64 x 4096 x 8192: 15.3 and 17.3.)  Up to four rows are read often at little cost (1 x 14336 x 4096 with 16, 32 and 64 rows of
+    // B: 8.9, 9.6, 9.6).
+    if (mode == kMxDense && m <= 64 && !(m > 32 && n < 160 * 32 && blocks > 320))
+        return {ProductPlan::kFew, 1, m <= 16 ? 1 : m <= 32 ? 2 : 4, m <= 4 && n < 160 * 128 ? 1 : few_nt((double)n)};
     // Rows of experts: every expert's matrix is read once in tiles, once for each 16 of its rows otherwise.  (Experts of 2048 x 4096, us
     // for few rows and in tiles: 64 experts with 2 rows each 48.5 and 55, with 4 60.6 and 59.8, with 16 90 and 62; 8 experts of
     // 4096 x 4096, too few tiles for the CUs, with 12 rows each 21.4 and 22.2, with 16 24.5 and 22.3.)
-    if (mode == kMxRows && m <= (std::min(m, experts) * ((n + 127) / 128) <= 512 ? 12 : 4) * experts) return {ProductPlan::kFew, 1};
-    const double stages = (double)((blocks + 7) / 8);
-    const int64_t batch = mode == kMxDepth ? experts : 1;
-    const int64_t large = ((m + 255) / 256) * ((n + 255) / 256) * batch, small = ((m + 127) / 128) * ((n + 127) / 128) * batch;
-    const int64_t rest = small % 512;
-    const int64_t left = large % 256;
-    const double in_large = (double)(large / 256) * (1.9 * stages + 8) +
+    if (mode == kMxRows && m <= (std::min<int64_t>(m, p.n_experts) * ((n + 127) / 128) <= 512 ? 12 : 4) * p.n_experts)
+        return {ProductPlan::kFew, 1, 1, std::min<int64_t>(m, p.n_experts) * n < 160 * 32 ? 1 : 2};
+    // Workgroups of 64 rows, if there are no more of them than CUs and the depth is not long (for few rows and in tiles, us of GPU time:
+    // 100 x 2700 x 2700 7.1 and 13.6, 128 x 4096 x 4096 10.4 and 16.0, 512 x 2048 x 2048 8.4 and 8.9; with 448 workgroups 128 x 14336 x
+    // 4096 24.5 and 20.8; with a depth of 8192 128 x 1024 x 8192 14.1 and 13.2).
+    if (mode != kMxDepth && blocks < 256) {
+        const double rows = tile_rows(mode, p, 64);
+        const int nt = few_nt(rows * n);
+        if (rows * (double)((n + 16 * nt - 1) / (16 * nt)) <= 256) return {ProductPlan::kFew, 1, 4, nt};
+    }
+    const double stages = std::ceil((double)blocks / 8 / (mode == kMxDepth ? std::max(p.n_experts, 1) : 1));
+    const double large = std::ceil(tile_rows(mode, p, 256) * (double)((n + 255) / 256)), small = std::ceil(tile_rows(mode, p, 128) * (double)((n + 127) / 128));
+    const double rest = std::fmod(small, 512), left = std::fmod(large, 256);
+    const double in_large = std::floor(large / 256) * (1.9 * stages + 8) +
                             (left == 0 ? 0.0 : left > 64 || large < 256 ? 1.9 * stages + 8 : 0.56 * stages + 5);
-    const double in_small = (double)(small / 512) * (1.29 * stages + 5) + (rest == 0 ? 0.0 : (rest <= 256 ? 0.56 : 1.29) * stages + 5);
-    if (in_large <= in_small) return {ProductPlan::kLargeTiles, 1};
+    const double in_small = std::floor(small / 512) * (1.29 * stages + 5) + (rest == 0 ? 0.0 : (rest <= 256 ? 0.56 : 1.29) * stages + 5);
+    if (in_large <= in_small) return {ProductPlan::kLargeTiles, 1, 0, 0};
     // Few tiles and a long depth: parts of it on idle CUs.  They are written and read again at about 4 TB/s, and joining them is a
     // launch of its own (128 x 4096 x 14336: 18.5 us in eight parts, 42 in one; 512 x 4096 x 4096: 18.2 in two, 13.9 in one).
-    ProductPlan best{ProductPlan::kSmallTiles, 1};
+    ProductPlan best{ProductPlan::kSmallTiles, 1, 0, 0};
     double least = in_small;
     if (mode == kMxDense && small <= 128)
         for (int splits = 2; splits * small <= 256 && splits <= 32; splits *= 2) {
@@ -850,8 +873,11 @@ static ProductPlan plan_product(int mode, int64_t m, int64_t n, int64_t blocks, 
 }
 static int64_t part_ld(int64_t n) { return (n + 3) / 4 * 4; }
 
-size_t mx_product_workspace(int64_t m, int64_t n, int64_t blocks) {
-    const int splits = plan_product(kMxDense, m, n, blocks, 1).splits;
+size_t mx_product_workspace(int64_t m, int64_t n, int32_t blocks) {
+    MxProductArgs p{};
+    p.m = m; p.n = n;
+    p.blocks = blocks;
+    const int splits = plan_product(kMxDense, p).splits;
     return splits == 1 ? 0 : (size_t)splits * m * part_ld(n) * 4;
 }
 
@@ -879,7 +905,7 @@ static hipError_t launch_few(int mode, const MxProductArgs& p, hipStream_t st) {
     if (n_tiles * m_tiles > 0x7FFFFFFFll) return hipErrorInvalidValue;
     const dim3 grid((uint32_t)(n_tiles * m_tiles)), block(kFewWaves * 64);
     if (mode == kMxDense) k_mx_few<kMxDense, MT, NT><<<grid, block, 0, st>>>(p, (uint32_t)n_tiles);
-    else if constexpr (MT == 1 && NT <= 2) k_mx_few<kMxRows, MT, NT><<<grid, block, 0, st>>>(p, (uint32_t)n_tiles);
+    else if constexpr (MT == 4 || (MT == 1 && NT <= 2)) k_mx_few<kMxRows, MT, NT><<<grid, block, 0, st>>>(p, (uint32_t)n_tiles);
     return hipGetLastError();
 }
 
@@ -897,19 +923,11 @@ static hipError_t launch_all_tiles(int mode, MxProductArgs p, bool large, hipStr
 hipError_t launch_mx_product(int mode, MxProductArgs p, void* workspace, hipStream_t st) {
     p.splits = 1;
     if (near_rows(p)) {
-        const ProductPlan plan = plan_product(mode, p.m, p.n, p.blocks, p.n_experts);
+        const ProductPlan plan = plan_product(mode, p);
         if (plan.kind == ProductPlan::kFew) {
-            if (mode == kMxRows) {
-                if (std::min<int64_t>(p.m, p.n_experts) * p.n < kFewNarrow * 32) return launch_few<1, 1>(mode, p, st);
-                return launch_few<1, 2>(mode, p, st);
-            }
-            // The more rows of B a workgroup takes, the less often A's are read (64 x 14336 x 4096: 30.5 us with 16, 18.6 with 32, 14.5
-            // with 64), which counts for little up to four (1 x 14336 x 4096: 8.9, 9.6, 9.6); but the CUs want enough workgroups
-            // (64 x 4096 x 4096: 8.6, 10.0, 13.4).
-            const int wide = p.n < kFewNarrow * 32 || (p.m <= 4 && p.n < kFewNarrow * 128) ? 1 : p.n < kFewNarrow * 64 ? 2 : 4;
-            if (p.m <= 16) return wide == 1 ? launch_few<1, 1>(mode, p, st) : wide == 2 ? launch_few<1, 2>(mode, p, st) : launch_few<1, 4>(mode, p, st);
-            if (p.m <= 32) return wide == 1 ? launch_few<2, 1>(mode, p, st) : wide == 2 ? launch_few<2, 2>(mode, p, st) : launch_few<2, 4>(mode, p, st);
-            return wide == 1 ? launch_few<4, 1>(mode, p, st) : wide == 2 ? launch_few<4, 2>(mode, p, st) : launch_few<4, 4>(mode, p, st);
+            if (plan.mt == 1) return plan.nt == 1 ? launch_few<1, 1>(mode, p, st) : plan.nt == 2 ? launch_few<1, 2>(mode, p, st) : launch_few<1, 4>(mode, p, st);
+            if (plan.mt == 2) return plan.nt == 1 ? launch_few<2, 1>(mode, p, st) : plan.nt == 2 ? launch_few<2, 2>(mode, p, st) : launch_few<2, 4>(mode, p, st);
+            return plan.nt == 1 ? launch_few<4, 1>(mode, p, st) : plan.nt == 2 ? launch_few<4, 2>(mode, p, st) : launch_few<4, 4>(mode, p, st);
         }
         if (plan.splits == 1) return launch_all_tiles(mode, p, plan.kind == ProductPlan::kLargeTiles, st);
         MxProductArgs part = p;
