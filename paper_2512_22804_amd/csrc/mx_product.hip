@@ -824,13 +824,15 @@ struct ProductPlan {
 // the CUs want 160 workgroups at least (64 x 4096 x 4096: 8.6, 10.0, 13.4).  `rows`: of B, times the workgroups for A's.
 static int few_nt(double rows) { return rows < 160 * 32 ? 1 : rows < 160 * 64 ? 2 : 4; }
 
-// Tiles of `height` rows: of a product, of all experts' results, or to expect in the segments of experts, which end in part tiles.
+// Tiles of `height` rows: of a product, of all experts' results, or to expect in the segments of experts, if the choices fall on them at
+// random: the mean of what a standard deviation less and one more choices for each would make.
 static double tile_rows(int mode, const MxProductArgs& p, int height) {
     if (mode != kMxRows) return (double)((p.m + height - 1) / height) * (mode == kMxDepth ? p.n_experts : 1);
-    const double used = std::max(std::min(p.n_experts, p.choices), 1);
-    const double each = std::max((double)p.choices / used + 0.5 * (p.align - 1), (double)p.align);      // rows with those that fill up
-    return std::min(used * std::max(each / height + (height > p.align ? 0.5 * (1.0 - (double)p.align / height) : 0.0), 1.0),
-                    (double)p.m / height + used);
+    const double used = std::max(std::min(p.n_experts, p.choices), 1), each = std::max((double)p.choices / used, 1.0);
+    double sum = 0;
+    for (const double rows : {std::max(each - std::sqrt(each), 1.0), each + std::sqrt(each)})
+        sum += std::ceil(std::ceil(rows / p.align) * p.align / height);
+    return used * sum / 2;
 }
 
 static ProductPlan plan_product(int mode, const MxProductArgs& p) {
