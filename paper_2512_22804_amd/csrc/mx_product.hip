@@ -533,16 +533,16 @@ struct Walk {
     }
 };
 
-// What the walk's present tile needs, or the quarter `piece` of a tile of twice the size (QUARTERS); false: nothing.
-template <int MODE, int BM, int BN, bool QUARTERS, class S>
+// What the walk's present tile needs, or piece `piece_of` of a tile of PIECES: 2, one above the other, or 4; false: nothing.
+template <int MODE, int BM, int BN, int PIECES, class S>
 __device__ __forceinline__ bool find_work(const MxProductArgs& p, const Walk& walk, uint32_t piece_of, int lane, int wave, TileWork<S>* w) {
     const uint32_t tall = min(8u, walk.m_tiles - walk.patch * 8), z = walk.z;
     uint32_t in_patch = walk.in_patch;
     const uint32_t n_tile = tall == 8 ? in_patch / 8 : in_patch / tall, m_tile = walk.patch * 8 + (in_patch - n_tile * tall);
     Tile& t = w->t;
-    if (!find_tile<MODE>(p, m_tile, z, QUARTERS ? 2 * BM : BM, &t)) return false;
-    w->n0 = (int64_t)n_tile * (QUARTERS ? 2 * BN : BN);
-    if (QUARTERS) {
+    if (!find_tile<MODE>(p, m_tile, z, PIECES > 1 ? 2 * BM : BM, &t)) return false;
+    w->n0 = (int64_t)n_tile * (PIECES == 4 ? 2 * BN : BN);
+    if (PIECES > 1) {
         t.m0 += (piece_of & 1) * BM;
         w->n0 += (piece_of >> 1) * BN;
         if (!__builtin_amdgcn_readfirstlane(t.m0 < t.m_end && w->n0 < p.n)) return false;
@@ -573,7 +573,7 @@ __device__ __forceinline__ bool find_work(const MxProductArgs& p, const Walk& wa
 
 // Workgroups stay and take tile after tile: the next tile's first stage is on its way while the sums go out by way of the second
 // buffer.
-template <int MODE, bool F32, int BM, int BN, bool QUARTERS>
+template <int MODE, bool F32, int BM, int BN, int PIECES>
 __device__ __forceinline__ void take_tiles(const MxProductArgs& p, Walk& walk, uint8_t* lds, uint32_t done) {
     typedef TileShape<BM, BN> S;
     constexpr int FM = S::FM, FN = S::FN;
@@ -599,10 +599,10 @@ __device__ __forceinline__ void take_tiles(const MxProductArgs& p, Walk& walk, u
     // this workgroup's first piece, the next one that is there
     uint32_t piece = walk.first;
     auto find = [&]() {
-        if (!QUARTERS) return find_work<MODE, BM, BN, false>(p, walk, 0u, lane, wave, &w);
+        if (PIECES == 1) return find_work<MODE, BM, BN, 1>(p, walk, 0u, lane, wave, &w);
         for (; walk.left; piece += walk.stride, walk.left = walk.left > walk.stride ? walk.left - walk.stride : 0u) {
-            walk.place(done + piece / 4, MODE != kMxRows, MODE == kMxDepth);
-            if (find_work<MODE, BM, BN, true>(p, walk, piece % 4, lane, wave, &w)) return true;
+            walk.place(done + piece / PIECES, MODE != kMxRows, MODE == kMxDepth);
+            if (find_work<MODE, BM, BN, PIECES>(p, walk, piece % PIECES, lane, wave, &w)) return true;
         }
         return false;
     };
@@ -655,7 +655,7 @@ __device__ __forceinline__ void take_tiles(const MxProductArgs& p, Walk& walk, u
         } while (++s < w.stages);
         // this tile's place in C, then the next tile
         const int64_t base = MODE != kMxRows ? w.t.expert * p.batch_c : 0, m0 = w.t.m0 + wm, m_end = w.t.m_end, n0 = w.n0 + wn;
-        if (QUARTERS) {
+        if (PIECES > 1) {
             piece += walk.stride;
             walk.left = walk.left > walk.stride ? walk.left - walk.stride : 0u;
         } else {
@@ -680,31 +680,30 @@ __device__ __forceinline__ void take_tiles(const MxProductArgs& p, Walk& walk, u
     }
 }
 
-// An XCD's workgroups take its tiles round by round.  If few are left for the last round (a quarter of the workgroups' number at most),
-// these are cut in quarters, one for each: 128 x 128 elements take 0.3 times as long as 256 x 256 (16384 rows of 16 experts, 2048 x 4096,
-// 2.25 rounds: 90 us, 102 without; two quarters for each would be slower than whole tiles for half of them: 6144 x 4096 x 8192,
-// 1.5 rounds: 126 us and 120).
+// An XCD's workgroups take its tiles round by round.  If few are left for the last round, they are cut in pieces, one for each workgroup at
+// most: in quarters or halves, which take 0.3 and 0.55 times as long as a whole tile.  (16384 rows of 16 experts, 2048 x 4096, 2.25
+// rounds: 90 us, 102 without; 6144 x 4096 x 8192, 1.5 rounds: 113 us, 120 without.)
 template <int MODE, bool F32, int BM, int BN, int GROUPS>
 __global__ __launch_bounds__(256, GROUPS) void k_mx_tile(MxProductArgs p, uint32_t total, uint32_t m_tiles, uint32_t n_tiles) {
-    constexpr bool kQuarters = GROUPS == 1;
+    constexpr bool kPieces = GROUPS == 1;
     __shared__ __align__(1024) uint8_t lds[TileShape<BM, BN>::kLds];
     if (MODE == kMxRows) {                              // the host knows no more than a bound of it
         m_tiles = count_rows(p, BM);
         total = m_tiles * n_tiles;
     }
     Walk walk(total, m_tiles, n_tiles, MODE == kMxDepth);
-    uint32_t rest = kQuarters ? walk.mine % walk.stride : 0u;
-    if (rest * 4 > walk.stride) rest = 0u;
-    const uint32_t whole = walk.mine - rest;
+    const uint32_t left = kPieces ? walk.mine % walk.stride : 0u, pieces = left * 4 <= walk.stride ? 4u : 2u;
+    const uint32_t rest = left * 2 <= walk.stride ? left : 0u, whole = walk.mine - rest;
     if (whole > walk.first) {
         walk.left = whole - walk.first;
         walk.place(walk.first, MODE != kMxRows, MODE == kMxDepth);
-        take_tiles<MODE, F32, BM, BN, false>(p, walk, lds, 0u);
+        take_tiles<MODE, F32, BM, BN, 1>(p, walk, lds, 0u);
     }
-    if (kQuarters && rest * 4 > walk.first) {
+    if (kPieces && rest * pieces > walk.first) {
         __syncthreads();
-        walk.left = rest * 4 - walk.first;
-        take_tiles<MODE, F32, BM / 2, BN / 2, true>(p, walk, lds, whole);
+        walk.left = rest * pieces - walk.first;
+        if (pieces == 4) take_tiles<MODE, F32, BM / 2, BN / 2, 4>(p, walk, lds, whole);
+        else take_tiles<MODE, F32, BM / 2, BN, 2>(p, walk, lds, whole);
     }
 }
 
@@ -813,7 +812,7 @@ __global__ __launch_bounds__(256) void k_mx_join(MxProductArgs p, const float* p
 }  // namespace
 
 // Which kernel a product of a given size takes.  Times in us, measured on whole and partly filled cards: a stage of a 256 x 256 tile
-// 1.9, of two 128 x 128 tiles on a CU 1.29, of one 0.56, and what a tile costs besides 8 and 5.  (In large tiles and in small ones,
+// 1.9, of half of one 1.05, of two 128 x 128 tiles on a CU 1.29, of one 0.56, and what a tile costs besides 8, 6 and 5.  (In large tiles and in small ones,
 // us: 4096 x 4096 x 4096 38 and 47, 4096 x 5120 x 512 16.8 and 17.4, 2048 x 4096 x 4096 30.1 and 27.6, 1024 x 4096 x 4096 27.9 and 17.1.)
 struct ProductPlan {
     enum { kFew, kSmallTiles, kLargeTiles } kind;
@@ -859,7 +858,7 @@ static ProductPlan plan_product(int mode, const MxProductArgs& p) {
     const double large = std::ceil(tile_rows(mode, p, 256) * (double)((n + 255) / 256)), small = std::ceil(tile_rows(mode, p, 128) * (double)((n + 127) / 128));
     const double rest = std::fmod(small, 512), left = std::fmod(large, 256);
     const double in_large = std::floor(large / 256) * (1.9 * stages + 8) +
-                            (left == 0 ? 0.0 : left > 64 || large < 256 ? 1.9 * stages + 8 : 0.56 * stages + 5);
+                            (left == 0 ? 0.0 : left > 128 || large < 256 ? 1.9 * stages + 8 : left > 64 ? 1.05 * stages + 6 : 0.56 * stages + 5);
     const double in_small = std::floor(small / 512) * (1.29 * stages + 5) + (rest == 0 ? 0.0 : (rest <= 256 ? 0.56 : 1.29) * stages + 5);
     if (in_large <= in_small) return {ProductPlan::kLargeTiles, 1, 0, 0};
     // Few tiles and a long depth: parts of it on idle CUs.  They are written and read again at about 4 TB/s, and joining them is a

@@ -112,3 +112,12 @@ def test_transposed_forms(batch, rows, cols, rounding):
             got = R.unpack_codes(op.codes[z].cpu().numpy(), op.codes.shape[-1] * 2)
             assert np.array_equal(got[:, :v.shape[1]], codes) and (got[:, v.shape[1]:] == 0).all()
             assert np.array_equal(op.scales[z].cpu().numpy()[:, :scales.shape[1]], scales)
+
+
+# 256 x 256 tiles whose last round is cut in halves: 24 x 16 (384), 16 x 23 with edges (a round and 112), 45 x 8 with an edge (104)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("m, n, k", [(6144, 4096, 300), (4090, 5802, 520), (11400, 2047, 96)])
+def test_tiles_in_halves(m, n, k, dtype):
+    a, av = random_operand(m, k, 14, spread=3)
+    b, bv = random_operand(n, k, 15, spread=3)
+    close(product(a, b, dtype), av, bv, dtype == torch.float32, k)
