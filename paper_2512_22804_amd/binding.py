@@ -177,15 +177,14 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # (not part of torch's public interface; neither is the next)
-_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # (not part of torch's public interface)
 
 
 def _stream():
     """Handle of the current device's current stream."""
     if _raw_stream is None:
         return torch.cuda.current_stream().cuda_stream
-    return _raw_stream(_device())
+    return _raw_stream(torch.cuda.current_device())
 
 
 @dataclass
