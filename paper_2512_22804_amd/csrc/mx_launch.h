@@ -12,8 +12,9 @@ constexpr int kMxBlock = 32;            // elements per scale
 // of whole lines, since parts of a line that go past the caches one by one are slower.  (De-quantisation of 14336 x 4096: 21.3 us
 // past the caches, 31.5 through them; of 18432 x 4104 40.4 and 28.2; of 4099 x 5001, which stays in the Infinity Cache, 14.1 and 12.8.)
 constexpr int64_t kMxStreamBytes = 1 << 26;
-inline bool mx_streamed(int64_t elements, const uint16_t* rows, int64_t ld, int64_t batch) {
-    return elements * 2 >= kMxStreamBytes && ((reinterpret_cast<uintptr_t>(rows) | (uintptr_t)(ld * 2) | (uintptr_t)(batch * 2)) & 127) == 0;
+constexpr int64_t kMxStreamReadBytes = 1 << 24;        // where only reads go past them (4096 x 4096 transposed: 11.1 us, 10.4 so)
+inline bool mx_streamed(int64_t elements, const uint16_t* rows, int64_t ld, int64_t batch, int64_t least = kMxStreamBytes) {
+    return elements * 2 >= least && ((reinterpret_cast<uintptr_t>(rows) | (uintptr_t)(ld * 2) | (uintptr_t)(batch * 2)) & 127) == 0;
 }
 
 // A packed operand on the device: codes and E8M0 bytes, leading dimensions and batch distances in bytes.

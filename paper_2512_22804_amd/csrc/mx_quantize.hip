@@ -292,7 +292,7 @@ hipError_t launch_mx_quantize(const MxQuantArgs& a, hipStream_t st) {
     if (tiles > 0x7FFFFFFFll) return hipErrorInvalidValue;
     const dim3 grid((uint32_t)tiles, 1, (uint32_t)a.batch);
     // rows gathered by expert are read several times; the rows form alone is no faster past the caches (19.1 us against 19.7)
-    const bool stream = t_form && a.src == nullptr && mx_streamed(a.rows * a.cols * a.batch, a.x, a.ld, a.batch_x);
+    const bool stream = t_form && a.src == nullptr && mx_streamed(a.rows * a.cols * a.batch, a.x, a.ld, a.batch_x, kMxStreamReadBytes);
     if (!t_form && tall) quantize_form<2, true, false, false>(a, col_tiles, grid, st);
     else if (!t_form) quantize_form<1, true, false, false>(a, col_tiles, grid, st);
     else if (short_t && rows_form) quantize_form<2, true, true, false>(a, col_tiles, grid, st);
