@@ -796,7 +796,8 @@ __global__ __launch_bounds__(kFewWaves * 64) void k_mx_few(MxProductArgs p, uint
     }
 }
 
-// Joins the parts of a split depth, in their order: four elements of a row per lane.
+// Joins the parts of a split depth, in their order: four elements of a row per lane.  Bound by its launch and the caches' latency (4 us
+// for eight parts of 128 x 4096).
 __global__ __launch_bounds__(256) void k_mx_join(MxProductArgs p, const float* parts, int64_t ld, int64_t batch, int splits) {
     const int64_t per_row = ld / 4, i = (int64_t)blockIdx.x * 256 + threadIdx.x, m = i / per_row, n = (i - m * per_row) * 4;
     if (m >= p.m || n >= p.n) return;
@@ -812,8 +813,9 @@ __global__ __launch_bounds__(256) void k_mx_join(MxProductArgs p, const float* p
 }  // namespace
 
 // Which kernel a product of a given size takes.  Times in us, measured on whole and partly filled cards: a stage of a 256 x 256 tile
-// 1.9, of half of one 1.05, of two 128 x 128 tiles on a CU 1.29, of one 0.56, and what a tile costs besides 8, 6 and 5.  (In large tiles and in small ones,
-// us: 4096 x 4096 x 4096 38 and 47, 4096 x 5120 x 512 16.8 and 17.4, 2048 x 4096 x 4096 30.1 and 27.6, 1024 x 4096 x 4096 27.9 and 17.1.)
+// 1.9, of half of one 1.05, of two 128 x 128 tiles on a CU 1.29, of one 0.56, and what a tile costs besides 8, 6 and 5.  (In large
+// tiles and in small ones, us: 4096 x 4096 x 4096 38 and 47, 4096 x 5120 x 512 16.8 and 17.4, 2048 x 4096 x 4096 30.1 and 27.6,
+// 1024 x 4096 x 4096 27.9 and 17.1.)
 struct ProductPlan {
     enum { kFew, kSmallTiles, kLargeTiles } kind;
     int splits;                         // parts of the depth
