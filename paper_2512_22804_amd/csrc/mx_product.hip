@@ -233,10 +233,12 @@ struct RowsBuffer {
 
 // 16 bytes per lane from a buffer straight into LDS, one lane behind the other from `lds` on.  Written out because the compiler
 // tracks the builtin's writes into LDS and, not being able to tell the four buffers apart across the loop, waits for all requests
-// before it reads any buffer.  Nothing is loaded into registers here, and the waits stand in multiply_stage.  (M0 is a reserved
-// register: the compiler sets it right before each use of its own, and nothing else in this kernel uses it.)
+// before it reads any buffer.  Nothing is loaded into registers here, and the waits stand in take_tiles.  (M0 is a reserved
+// register: the compiler sets it right before each use of its own, and nothing else in this kernel uses it.)  Nor does the compiler
+// look into the text for wait states: five must lie between a vector instruction that writes a scalar register (v_readfirstlane, or
+// v_readlane where one was spilled) and a buffer load that reads it, so they stand here, whatever comes before.
 __device__ __forceinline__ void load_to_lds(uint32_t lds, u32x4 buffer, uint32_t offset) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(lds), "v"(offset), "s"(buffer) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(lds), "v"(offset), "s"(buffer) : "memory");
 }
 
 template <int BM, int BN>
@@ -258,12 +260,21 @@ struct Request {
 };
 
 // Wave w loads the codes of rows 8 (w + 4 i) .. + 7 of one stage: request `i` of A's, then B's.
+struct Asked {
+    u32x4 buffer;
+    uint32_t lds, offset;
+};
 template <class S>
-__device__ __forceinline__ void request_codes(uint32_t lds, const Request& q, int stage, int wave, int i) {
+__device__ __forceinline__ Asked codes_request(uint32_t lds, const Request& q, int stage, int wave, int i) {
     constexpr int kOfA = S::kCodesB / 4096;
     const bool exists = stage <= q.last;
-    if (i < kOfA) load_to_lds(lds + (wave + 4 * i) * 1024, q.a.at(stage * 128, exists), (stage == q.last ? q.va_last : q.va) + i * q.step_a);
-    else load_to_lds(lds + S::kCodesB + (wave + 4 * (i - kOfA)) * 1024, q.b.at(stage * 128, exists), (stage == q.last ? q.vb_last : q.vb) + (i - kOfA) * q.step_b);
+    if (i < kOfA) return {q.a.at(stage * 128, exists), lds + (wave + 4 * i) * 1024, (stage == q.last ? q.va_last : q.va) + i * q.step_a};
+    return {q.b.at(stage * 128, exists), lds + S::kCodesB + (wave + 4 * (i - kOfA)) * 1024, (stage == q.last ? q.vb_last : q.vb) + (i - kOfA) * q.step_b};
+}
+template <class S>
+__device__ __forceinline__ void request_codes(uint32_t lds, const Request& q, int stage, int wave, int i) {
+    const Asked r = codes_request<S>(lds, q, stage, wave, i);
+    load_to_lds(r.lds, r.buffer, r.offset);
 }
 // The scales of two stages, 16 bytes of a row.  Wave w loads those of rows 64 w .. + 63 of either operand; where one has fewer, several
 // waves load the same.
@@ -333,6 +344,21 @@ __device__ __forceinline__ void multiply(f32x16& c, u32x4 b, uint32_t sb, u32x4 
         asm("s_nop 1\n\tv_mfma_scale_f32_32x32x64_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[0,0,0] op_sel_hi:[1,1,0] cbsz:4 blgp:4"
             : "+a"(c) : "v"(b), "v"(a), "v"(sb), "v"(sa));
 }
+// The same and load_to_lds behind it.  The matrix instruction and the states before it are four of the five that the request wants
+// (8192 x 14336 x 4096: 247 us, as long as with two states before each request; 250 with five in a text of their own).
+template <int STEP>
+__device__ __forceinline__ void multiply_and_request(f32x16& c, u32x4 b, uint32_t sb, u32x4 a, uint32_t sa, const Asked& r) {
+    if (STEP == 0)
+        asm volatile("s_mov_b32 m0, %5\n\ts_nop 2\n\t"
+                     "v_mfma_scale_f32_32x32x64_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[0,0,0] op_sel_hi:[0,0,0] cbsz:4 blgp:4\n\t"
+                     "buffer_load_dwordx4 %6, %7, 0 offen lds"
+                     : "+a"(c) : "v"(b), "v"(a), "v"(sb), "v"(sa), "s"(r.lds), "v"(r.offset), "s"(r.buffer) : "memory");
+    else
+        asm volatile("s_mov_b32 m0, %5\n\ts_nop 2\n\t"
+                     "v_mfma_scale_f32_32x32x64_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[0,0,0] op_sel_hi:[1,1,0] cbsz:4 blgp:4\n\t"
+                     "buffer_load_dwordx4 %6, %7, 0 offen lds"
+                     : "+a"(c) : "v"(b), "v"(a), "v"(sb), "v"(sa), "s"(r.lds), "v"(r.offset), "s"(r.buffer) : "memory");
+}
 // Before the first other use of the sums: the last matrix instruction (eight passes of four cycles) has written its own.
 template <int FM, int FN>
 __device__ __forceinline__ void settle(f32x16 (&acc)[FM][FN]) {
@@ -356,12 +382,19 @@ __device__ __forceinline__ void multiply_step(f32x16 (&acc)[S::FM][S::FN], const
     constexpr int FM = S::FM, FN = S::FN, kSlots = FM * FN, kWord = STEP / 2;
     constexpr int kFirst = S::kFirstRequests, kFrom = STEP == 3 ? 0 : kFirst;
     constexpr int kCount = STEP == 3 ? kFirst : STEP == 0 ? S::kRequests - kFirst : 0;
+    static_assert(kCount <= kSlots, "one request behind a matrix instruction");
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
             const int slot = i * FN + j;
-            multiply<STEP % 2>(acc[i][j], cur.b[j], scales.b[j][kWord], cur.a[i], scales.a[i][kWord]);
+            int asked = -1;                             // at most one request behind a matrix instruction
+#pragma unroll
+            for (int r = 0; r < kCount; ++r)
+                if (slot == r * kSlots / (kCount ? kCount : 1)) asked = r;
+            if (asked < 0) multiply<STEP % 2>(acc[i][j], cur.b[j], scales.b[j][kWord], cur.a[i], scales.a[i][kWord]);
+            else multiply_and_request<STEP % 2>(acc[i][j], cur.b[j], scales.b[j][kWord], cur.a[i], scales.a[i][kWord],
+                                                codes_request<S>(to, q, ahead, wave, kFrom + asked));
             // the reads over the first half of the slots, so that they are complete by the end
 #pragma unroll
             for (int r = 0; r < FM + FN; ++r)
@@ -369,9 +402,6 @@ __device__ __forceinline__ void multiply_step(f32x16 (&acc)[S::FM][S::FN], const
                     if (r < FN) next.b[r] = *reinterpret_cast<const u32x4*>(next_b + r * 4096);
                     else next.a[r - FN] = *reinterpret_cast<const u32x4*>(next_a + (r - FN) * 4096);
                 }
-#pragma unroll
-            for (int r = 0; r < kCount; ++r)
-                if (slot == r * kSlots / (kCount ? kCount : 1)) request_codes<S>(to, q, ahead, wave, kFrom + r);
             if (STEP == 3) {
                 if (j == 0) fresh.a[i] = *reinterpret_cast<const u32x2*>(scales_a + i * 512);
                 if (i == 0) fresh.b[j] = *reinterpret_cast<const u32x2*>(scales_b + j * 512);
@@ -699,11 +729,13 @@ __global__ __launch_bounds__(256, GROUPS) void k_mx_tile(MxProductArgs p, uint32
         walk.place(walk.first, MODE != kMxRows, MODE == kMxDepth);
         take_tiles<MODE, F32, BM, BN, 1>(p, walk, lds, 0u);
     }
-    if (kPieces && rest * pieces > walk.first) {
-        __syncthreads();
-        walk.left = rest * pieces - walk.first;
-        if (pieces == 4) take_tiles<MODE, F32, BM / 2, BN / 2, 4>(p, walk, lds, whole);
-        else take_tiles<MODE, F32, BM / 2, BN, 2>(p, walk, lds, whole);
+    if constexpr (kPieces) {
+        if (rest * pieces > walk.first) {
+            __syncthreads();
+            walk.left = rest * pieces - walk.first;
+            if (pieces == 4) take_tiles<MODE, F32, BM / 2, BN / 2, 4>(p, walk, lds, whole);
+            else take_tiles<MODE, F32, BM / 2, BN, 2>(p, walk, lds, whole);
+        }
     }
 }
 
