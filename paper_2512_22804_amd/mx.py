@@ -2,7 +2,8 @@
 declared in ``include/mor_mx.h``, exported by ``libmor.so``).
 
 Argument marshalling only, as in :mod:`binding`: tensors are checked for what the C ABI cannot see (device, type, shape,
-strides), and every call raises :class:`binding.MorError` for what it refuses.  Calls are enqueued on the current stream.
+strides), and every call raises :class:`binding.MorError` for what it refuses.  What a call takes lives on one device; it is enqueued on
+that device's current stream.
 """
 from __future__ import annotations
 
@@ -70,7 +71,29 @@ def load():
     return _lib
 
 
-def _check(rc: int, where: str) -> None:
+def _device(where: str, *things) -> int:
+    """Index of the device that all of ``things`` (tensors, operands, orders; None: not there) live on."""
+    device = None
+    for t in things:
+        if t is not None:
+            index = t.get_device()
+            if index < 0:
+                raise ValueError(f"{where}: all tensors must live in device memory")
+            if index != device:
+                if device is not None:
+                    raise ValueError(f"{where}: tensors on devices {device} and {index}")
+                device = index
+    return device
+
+
+def _run(where: str, device: int, *args) -> None:
+    """Calls the library with ``device`` as the current one and its current stream."""
+    call = getattr(load(), where)
+    if device == torch.cuda.current_device():
+        rc = call(*args, binding._stream())
+    else:
+        with torch.cuda.device(device):
+            rc = call(*args, binding._stream())
     if rc != 0:
         raise binding.MorError(rc, where)
 
@@ -117,6 +140,7 @@ class MxOperand:
             raise ValueError("codes and scales must live on one device")
         lone = self.rows == 1
         object.__setattr__(self, "batch", self.codes.shape[0] if self.codes.dim() == 3 else 1)
+        object.__setattr__(self, "_index", self.codes.get_device())
         object.__setattr__(self, "_struct", MorMxOperand(
             None, self.codes.shape[-1] if lone else self.codes.stride(-2), None, self.scales.shape[-1] if lone else self.scales.stride(-2),
             self.codes.stride(0) if self.codes.dim() == 3 else 0, self.scales.stride(0) if self.scales.dim() == 3 else 0))
@@ -125,10 +149,11 @@ class MxOperand:
     def blocks(self) -> int:
         return -(-self.cols // BLOCK)
 
+    def get_device(self) -> int:
+        return self._index
+
     def struct(self) -> int:
         """Address of the operand's structure, valid as long as the operand."""
-        if not self.codes.is_cuda:
-            raise ValueError("the operand must live in device memory")
         struct = self._struct
         struct.codes, struct.scales = self.codes.data_ptr(), self.scales.data_ptr()
         return C.addressof(struct)
@@ -158,7 +183,11 @@ class ExpertOrder:
         _vector(self.offsets, "offsets", torch.int32, self.n_experts + 1)
         _vector(self.slot_of, "slot_of", torch.int32, self.tokens * self.top_k)
         _vector(self.src, "src", torch.int32, self.capacity)
+        object.__setattr__(self, "_index", _device("ExpertOrder", self.offsets, self.slot_of, self.src, self.workspace))
         object.__setattr__(self, "_struct", MorExpertOrder(self.tokens, self.top_k, self.n_experts, self.align, self.capacity, 0))
+
+    def get_device(self) -> int:
+        return self._index
 
     def struct(self) -> int:
         """Address of the order's structure, valid as long as the order."""
@@ -199,10 +228,9 @@ def mor_mx_quantize(x: torch.Tensor, out: MxOperand | None = None, out_t: MxOper
         if operand is not None and ((operand.rows, operand.cols) != shape or operand.batch != batch):
             raise ValueError(f"{name} must be {batch} operand(s) of {shape[0]} x {shape[1]}")
     params = MorMxParams(rows, cols, ld, batch, batch_x, SCALE_RULE[scale_rule], ROUNDING[rounding], seed & 0xFFFFFFFFFFFFFFFF)
-    _check(load().mor_mx_quantize(C.addressof(params), x.data_ptr(), out.struct() if out is not None else None,
-                                  out_t.struct() if out_t is not None else None,
-                                  order.struct() if order is not None else None, binding._ptr(weights), binding._stream()),
-           "mor_mx_quantize")
+    _run("mor_mx_quantize", _device("mor_mx_quantize", x, out, out_t, order, weights), C.addressof(params), x.data_ptr(),
+         out.struct() if out is not None else None, out_t.struct() if out_t is not None else None,
+         order.struct() if order is not None else None, binding._ptr(weights))
 
 
 def mor_mx_dequantize(operand: MxOperand, y: torch.Tensor) -> None:
@@ -211,8 +239,8 @@ def mor_mx_dequantize(operand: MxOperand, y: torch.Tensor) -> None:
     batch, batch_y = _batch(y)
     if y.shape[-2:] != (operand.rows, operand.cols) or batch != operand.batch:
         raise ValueError(f"y must be {operand.batch} matrices of {operand.rows} x {operand.cols}")
-    _check(load().mor_mx_dequantize(operand.rows, operand.cols, batch, operand.struct(), y.data_ptr(), ld, batch_y,
-                                    binding._stream()), "mor_mx_dequantize")
+    _run("mor_mx_dequantize", _device("mor_mx_dequantize", operand, y), operand.rows, operand.cols, batch, operand.struct(),
+         y.data_ptr(), ld, batch_y)
 
 
 _OUT = {torch.bfloat16: 0, torch.float32: 1}
@@ -233,9 +261,8 @@ def mor_mx_product(a: MxOperand, b: MxOperand, c: torch.Tensor, workspace: torch
     ld = _matrix(c, "c", _OUT)
     if a.cols != b.cols or a.batch != 1 or b.batch != 1 or c.shape != (a.rows, b.rows):
         raise ValueError(f"shapes do not match: {a.rows} x {a.cols}, {b.rows} x {b.cols}, result {tuple(c.shape)}")
-    _check(load().mor_mx_product(a.rows, b.rows, a.cols, a.struct(), b.struct(), c.data_ptr(), ld, _OUT[c.dtype],
-                                 binding._ptr(workspace), workspace.numel() if workspace is not None else 0, binding._stream()),
-           "mor_mx_product")
+    _run("mor_mx_product", _device("mor_mx_product", a, b, c, workspace), a.rows, b.rows, a.cols, a.struct(), b.struct(), c.data_ptr(), ld,
+         _OUT[c.dtype], binding._ptr(workspace), workspace.numel() if workspace is not None else 0)
 
 
 def mor_mx_product_rows(a: MxOperand, b: MxOperand, order: ExpertOrder, c: torch.Tensor) -> None:
@@ -244,8 +271,8 @@ def mor_mx_product_rows(a: MxOperand, b: MxOperand, order: ExpertOrder, c: torch
     if a.cols != b.cols or a.batch != 1 or a.rows != order.capacity or b.batch != order.n_experts or c.shape != (a.rows, b.rows):
         raise ValueError(f"shapes do not match: {a.rows} x {a.cols}, {b.batch} of {b.rows} x {b.cols}, {order.n_experts} experts, "
                          f"{order.capacity} slots, result {tuple(c.shape)}")
-    _check(load().mor_mx_product_rows(b.rows, a.cols, a.struct(), b.struct(), order.struct(), c.data_ptr(), ld,
-                                      _OUT[c.dtype], binding._stream()), "mor_mx_product_rows")
+    _run("mor_mx_product_rows", _device("mor_mx_product_rows", a, b, order, c), b.rows, a.cols, a.struct(), b.struct(), order.struct(),
+         c.data_ptr(), ld, _OUT[c.dtype])
 
 
 def mor_mx_product_depth(a: MxOperand, b: MxOperand, order: ExpertOrder, c: torch.Tensor) -> None:
@@ -255,16 +282,16 @@ def mor_mx_product_depth(a: MxOperand, b: MxOperand, order: ExpertOrder, c: torc
             c.dim() != 3 or c.shape != (order.n_experts, a.rows, b.rows):
         raise ValueError(f"shapes do not match: {a.rows} x {a.cols}, {b.rows} x {b.cols}, {order.n_experts} experts, "
                          f"{order.capacity} slots, result {tuple(c.shape)}")
-    _check(load().mor_mx_product_depth(a.rows, b.rows, a.struct(), b.struct(), order.struct(), c.data_ptr(), ld,
-                                       _batch(c)[1], _OUT[c.dtype], binding._stream()), "mor_mx_product_depth")
+    _run("mor_mx_product_depth", _device("mor_mx_product_depth", a, b, order, c), a.rows, b.rows, a.struct(), b.struct(), order.struct(),
+         c.data_ptr(), ld, _batch(c)[1], _OUT[c.dtype])
 
 
 def mor_expert_sort(ids: torch.Tensor, order: ExpertOrder) -> None:
     """``ids`` (tokens, top_k) int32: the expert of each choice; outside [0, n_experts): dropped."""
     _vector(ids, "ids", torch.int32, order.tokens * order.top_k)
     ws = order.workspace
-    _check(load().mor_expert_sort(ids.data_ptr(), order.struct(), binding._ptr(ws), ws.numel() if ws is not None else 0,
-                                  binding._stream()), "mor_expert_sort")
+    _run("mor_expert_sort", _device("mor_expert_sort", ids, order), ids.data_ptr(), order.struct(), binding._ptr(ws),
+         ws.numel() if ws is not None else 0)
 
 
 def _rows(t: torch.Tensor | None, name: str, rows: int, d: int) -> int:
@@ -280,8 +307,7 @@ def mor_expert_gather(x: torch.Tensor, order: ExpertOrder, xs: torch.Tensor) -> 
     """``xs`` (capacity, d): the token's row for every slot, zeros for empty ones."""
     d = x.shape[-1]
     ld_x, ld_xs = _rows(x, "x", order.tokens, d), _rows(xs, "xs", order.capacity, d)
-    _check(load().mor_expert_gather(x.data_ptr(), ld_x, d, order.struct(), xs.data_ptr(), ld_xs, binding._stream()),
-           "mor_expert_gather")
+    _run("mor_expert_gather", _device("mor_expert_gather", x, order, xs), x.data_ptr(), ld_x, d, order.struct(), xs.data_ptr(), ld_xs)
 
 
 def mor_expert_combine(ys: torch.Tensor, order: ExpertOrder, weights: torch.Tensor | None, y: torch.Tensor) -> None:
@@ -289,8 +315,8 @@ def mor_expert_combine(ys: torch.Tensor, order: ExpertOrder, weights: torch.Tens
     d = ys.shape[-1]
     ld_ys, ld_y = _rows(ys, "ys", order.capacity, d), _rows(y, "y", order.tokens, d)
     _vector(weights, "weights", torch.float32, order.tokens * order.top_k)
-    _check(load().mor_expert_combine(ys.data_ptr(), ld_ys, d, order.struct(), binding._ptr(weights), y.data_ptr(), ld_y, binding._stream()),
-           "mor_expert_combine")
+    _run("mor_expert_combine", _device("mor_expert_combine", ys, order, weights, y), ys.data_ptr(), ld_ys, d, order.struct(),
+         binding._ptr(weights), y.data_ptr(), ld_y)
 
 
 def mor_expert_combine_backward(dy: torch.Tensor, ys: torch.Tensor | None, order: ExpertOrder, weights: torch.Tensor | None,
@@ -300,6 +326,5 @@ def mor_expert_combine_backward(dy: torch.Tensor, ys: torch.Tensor | None, order
     ld_dy, ld_ys, ld_dys = _rows(dy, "dy", order.tokens, d), _rows(ys, "ys", order.capacity, d), _rows(dys, "dys", order.capacity, d)
     _vector(weights, "weights", torch.float32, order.tokens * order.top_k)
     _vector(dweights, "dweights", torch.float32, order.tokens * order.top_k)
-    _check(load().mor_expert_combine_backward(dy.data_ptr(), ld_dy, binding._ptr(ys), ld_ys, d, order.struct(), binding._ptr(weights),
-                                              binding._ptr(dys), ld_dys, binding._ptr(dweights), binding._stream()),
-           "mor_expert_combine_backward")
+    _run("mor_expert_combine_backward", _device("mor_expert_combine_backward", dy, ys, order, weights, dys, dweights), dy.data_ptr(), ld_dy,
+         binding._ptr(ys), ld_ys, d, order.struct(), binding._ptr(weights), binding._ptr(dys), ld_dys, binding._ptr(dweights))
