@@ -906,8 +906,10 @@ static ProductPlan plan_product(int mode, const MxProductArgs& p) {
         }
     // Parts of whole stages: no more of them than get any (100 x 257 x 8200: 33 stages in 11 parts of three, not in 16).  The first block
     // of each is then a multiple of 8, so that its scales begin at a whole word.
-    const int all = (blocks + 7) / 8, each = (all + best.splits - 1) / best.splits;
-    best.splits = (all + each - 1) / each;
+    if (best.splits > 1) {
+        const int all = (int)((blocks + 7) / 8), each = (all + best.splits - 1) / best.splits;
+        best.splits = (all + each - 1) / each;
+    }
     return best;
 }
 static int64_t part_ld(int64_t n) { return (n + 3) / 4 * 4; }

@@ -1,6 +1,9 @@
 """A product whose depth is split over workgroups (no kernel is launched): every part has some of the depth.  One without would read its
 scales from an address that is no whole word, write zeros and have them read back."""
+import ctypes as C
+
 import pytest
+import torch
 
 from paper_2512_22804_amd import mx
 
@@ -25,3 +28,13 @@ def test_no_part_is_empty(m, n, k):
 
 def test_these_are_split():
     assert all(parts(*size) > 1 for size in ((100, 257, 8200), (128, 128, 9000), (128, 4096, 14336), (65, 65, 100000)))
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="the addresses are made up: nothing may be launched")
+def test_no_depth_at_all():
+    """A product over the experts' depth without a slot: nothing to split.  Without a GPU the launch fails; the plan before it must not divide
+    by the number of stages."""
+    order = mx.MorExpertOrder(0, 2, 3, 128, 0, 0, 1 << 40, None, None)
+    op = mx.MorMxOperand(1 << 40, 16, 1 << 40, 4, 0, 0)
+    status = mx.load().mor_mx_product_depth(8, 8, C.byref(op), C.byref(op), C.byref(order), 1 << 40, 8, 64, 0, None)
+    assert status in (0, 6)
