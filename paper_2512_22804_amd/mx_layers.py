@@ -25,6 +25,13 @@ def _check(x: torch.Tensor, w: torch.Tensor, dims: int) -> None:
         raise ValueError(f"shapes do not match: x {tuple(x.shape)}, w {tuple(w.shape)}")
 
 
+def _seed(seed: int | None, rounds: bool) -> int:
+    """The seed of a call's gradients; without one of the caller's a new one, if there is a gradient to round at all."""
+    if seed is None:
+        seed = int(torch.randint(1 << 62, ())) if rounds else 0
+    return seed
+
+
 def _product(a: mx.MxOperand, b: mx.MxOperand, dtype: torch.dtype) -> torch.Tensor:
     if a.cols == 0:                     # no tokens: a gradient without terms
         return torch.zeros(a.rows, b.rows, dtype=dtype, device=a.codes.device)
@@ -60,11 +67,13 @@ class _Linear(torch.autograd.Function):
         return dx, dw, None, None, None
 
 
-def linear(x: torch.Tensor, w: torch.Tensor, scale_rule: str = "floor", seed: int = 0) -> torch.Tensor:
+def linear(x: torch.Tensor, w: torch.Tensor, scale_rule: str = "floor", seed: int | None = None) -> torch.Tensor:
     """``x`` (tokens, hidden) times ``w`` (width, hidden), transposed, in BF16.  ``x`` and ``w`` are BF16 or float32, which their gradients then
-    are too.  ``seed``: of the gradients' rounding, another one each step and layer."""
+    are too.  ``seed``: of the gradients' rounding, another one each step and layer; None: every call draws one from torch's generator on
+    the host (a captured graph repeats the one that was drawn)."""
     _check(x, w, 2)
-    return _Linear.apply(x, w, scale_rule, seed, torch.is_grad_enabled())
+    training = torch.is_grad_enabled()
+    return _Linear.apply(x, w, scale_rule, _seed(seed, training and (x.requires_grad or w.requires_grad)), training)
 
 
 class _Experts(torch.autograd.Function):
@@ -110,11 +119,14 @@ class _Experts(torch.autograd.Function):
         return dx, dw, None, dweights, None, None, None
 
 
-def experts(x: torch.Tensor, w: torch.Tensor, ids: torch.Tensor, weights: torch.Tensor, scale_rule: str = "floor", seed: int = 0) -> torch.Tensor:
+def experts(x: torch.Tensor, w: torch.Tensor, ids: torch.Tensor, weights: torch.Tensor, scale_rule: str = "floor",
+            seed: int | None = None) -> torch.Tensor:
     """Sum over a token's choices ``ids`` (tokens, top_k; int32, outside the experts: dropped) of its ``weights`` (tokens, top_k; float32) times
-    the token's row of ``x`` (tokens, hidden) times that expert's matrix of ``w`` (experts, width, hidden), transposed; in BF16."""
+    the token's row of ``x`` (tokens, hidden) times that expert's matrix of ``w`` (experts, width, hidden), transposed; in BF16.  ``seed``
+    as for :func:`linear`."""
     _check(x, w, 3)
-    return _Experts.apply(x, w, ids, weights, scale_rule, seed, torch.is_grad_enabled())
+    training = torch.is_grad_enabled()
+    return _Experts.apply(x, w, ids, weights, scale_rule, _seed(seed, training and (x.requires_grad or w.requires_grad)), training)
 
 
 class ServedExperts:
