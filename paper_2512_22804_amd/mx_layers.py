@@ -3,7 +3,9 @@ their form without for serving.  ``python -m paper_2512_22804_amd.mx_layers`` tr
 
 Every product reads 4-bit operands whose blocks lie along its depth, so an operand of a training step is quantised in two forms from
 one read: as it is and transposed.  Activations and weights are rounded to nearest, gradients stochastically, whose errors
-average out over steps.  What is quantised in the forward pass for the backward pass is kept in 4 bits, not in 16.
+average out over steps, if nothing is clipped: under the floor rule magnitudes in (6, 8) times a block's scale become 6 times it
+whatever the random bits (the mean over draws of normal numbers is off by 4 % of their norm), under the ceil rule none does.  What is quantised in the
+forward pass for the backward pass is kept in 4 bits, not in 16.
 """
 from __future__ import annotations
 
@@ -25,11 +27,16 @@ def _check(x: torch.Tensor, w: torch.Tensor, dims: int) -> None:
         raise ValueError(f"shapes do not match: x {tuple(x.shape)}, w {tuple(w.shape)}")
 
 
-def _seed(seed: int | None, rounds: bool) -> int:
-    """The seed of a call's gradients; without one of the caller's a new one, if there is a gradient to round at all."""
+def _gradients(scale_rule: str, seed: int | None, gradient_rule: str | None, rounds: bool) -> dict:
+    """How a call's gradients are rounded.  Without a seed of the caller's it is a new one, if there is a gradient to round at all."""
+    if gradient_rule is None:
+        gradient_rule = "ceil" if seed is None else scale_rule
+    for rule in (scale_rule, gradient_rule):
+        if rule not in mx.SCALE_RULE:
+            raise ValueError(f"{rule!r} is not one of {tuple(mx.SCALE_RULE)}")
     if seed is None:
         seed = int(torch.randint(1 << 62, ())) if rounds else 0
-    return seed
+    return dict(scale_rule=gradient_rule, rounding="stochastic", seed=seed)
 
 
 def _product(a: mx.MxOperand, b: mx.MxOperand, dtype: torch.dtype) -> torch.Tensor:
@@ -50,12 +57,12 @@ def _operands(x: torch.Tensor, rows: int, cols: int, transposed: bool = True, ba
 
 class _Linear(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, w, scale_rule, seed, training):
+    def forward(ctx, x, w, scale_rule, how, training):
         tokens, hidden = x.shape
         # either input's transpose is what the other one's gradient reads
         xq, xt = _operands(_bf16(x), tokens, hidden, training and ctx.needs_input_grad[1], scale_rule=scale_rule)
         wq, wt = _operands(_bf16(w), w.shape[0], hidden, training and ctx.needs_input_grad[0], scale_rule=scale_rule)
-        ctx.operands, ctx.how, ctx.types = (xt, wt), dict(scale_rule=scale_rule, rounding="stochastic", seed=seed), (x.dtype, w.dtype)
+        ctx.operands, ctx.how, ctx.types = (xt, wt), how, (x.dtype, w.dtype)
         return _product(xq, wq, torch.bfloat16)
 
     @staticmethod
@@ -67,18 +74,23 @@ class _Linear(torch.autograd.Function):
         return dx, dw, None, None, None
 
 
-def linear(x: torch.Tensor, w: torch.Tensor, scale_rule: str = "floor", seed: int | None = None) -> torch.Tensor:
+def linear(x: torch.Tensor, w: torch.Tensor, scale_rule: str = "floor", seed: int | None = None, gradient_rule: str | None = None) -> torch.Tensor:
     """``x`` (tokens, hidden) times ``w`` (width, hidden), transposed, in BF16.  ``x`` and ``w`` are BF16 or float32, which their gradients then
-    are too.  ``seed``: of the gradients' rounding, another one each step and layer; None: every call draws one from torch's generator on
-    the host (a captured graph repeats the one that was drawn)."""
+    are too.
+
+    ``seed``: of the gradients' rounding, another one each step and layer; None: every call draws one from torch's generator on
+    the host (a captured graph repeats the one that was drawn).  ``gradient_rule``: the scale rule of the gradients, "ceil" for rounding
+    without bias, which is what a call without a seed does; with a seed it is ``scale_rule`` unless given, so that such
+    calls repeat what they have always answered."""
     _check(x, w, 2)
     training = torch.is_grad_enabled()
-    return _Linear.apply(x, w, scale_rule, _seed(seed, training and (x.requires_grad or w.requires_grad)), training)
+    how = _gradients(scale_rule, seed, gradient_rule, training and (x.requires_grad or w.requires_grad))
+    return _Linear.apply(x, w, scale_rule, how, training)
 
 
 class _Experts(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, w, ids, weights, scale_rule, seed, training):
+    def forward(ctx, x, w, ids, weights, scale_rule, how, training):
         tokens, hidden = x.shape
         experts, width = w.shape[:2]
         # segments of whole 128 rows: the matrices' gradients are sums over them
@@ -92,7 +104,7 @@ class _Experts(torch.autograd.Function):
         weights = weights.detach().contiguous()
         mx.mor_expert_combine(ys, order, weights, y)
         ctx.save_for_backward(weights)
-        ctx.kept, ctx.how, ctx.types = (order, xt, wt, ys), dict(scale_rule=scale_rule, rounding="stochastic", seed=seed), (x.dtype, w.dtype)
+        ctx.kept, ctx.how, ctx.types = (order, xt, wt, ys), how, (x.dtype, w.dtype)
         return y
 
     @staticmethod
@@ -120,13 +132,14 @@ class _Experts(torch.autograd.Function):
 
 
 def experts(x: torch.Tensor, w: torch.Tensor, ids: torch.Tensor, weights: torch.Tensor, scale_rule: str = "floor",
-            seed: int | None = None) -> torch.Tensor:
+            seed: int | None = None, gradient_rule: str | None = None) -> torch.Tensor:
     """Sum over a token's choices ``ids`` (tokens, top_k; int32, outside the experts: dropped) of its ``weights`` (tokens, top_k; float32) times
     the token's row of ``x`` (tokens, hidden) times that expert's matrix of ``w`` (experts, width, hidden), transposed; in BF16.  ``seed``
-    as for :func:`linear`."""
+    and ``gradient_rule`` as for :func:`linear`."""
     _check(x, w, 3)
     training = torch.is_grad_enabled()
-    return _Experts.apply(x, w, ids, weights, scale_rule, _seed(seed, training and (x.requires_grad or w.requires_grad)), training)
+    how = _gradients(scale_rule, seed, gradient_rule, training and (x.requires_grad or w.requires_grad))
+    return _Experts.apply(x, w, ids, weights, scale_rule, how, training)
 
 
 class ServedExperts:
@@ -158,9 +171,9 @@ def train(steps: int = 60, tokens: int = 512, hidden: int = 256, width: int = 19
     optimizer = torch.optim.Adam(mine, lr=2e-3)
 
     def answer(x, params, ids, seed):
-        h = linear(x, params[0], seed=seed)
+        h = linear(x, params[0], seed=seed, gradient_rule="ceil")
         chosen = (x.float() @ params[2].t()).gather(1, ids.long()).softmax(dim=1)
-        return experts(h, params[1], ids, chosen, seed=seed + 1)
+        return experts(h, params[1], ids, chosen, seed=seed + 1, gradient_rule="ceil")
 
     losses = []
     for step in range(steps):

@@ -58,3 +58,38 @@ def test_random_bits(kind):
     with torch.no_grad():
         answer(kind, x.clone().requires_grad_(), w, args)
     assert torch.equal(before, torch.get_rng_state())
+
+
+@pytest.mark.parametrize("how", [{}, {"gradient_rule": "ceil", "seed": 1}])
+@pytest.mark.parametrize("kind", ["linear", "experts"])
+def test_gradients_have_no_bias(kind, how):
+    """Every rounding error E of dy has a step of 2 at most (scale 2, magnitudes below 8), so a mean of zero and a variance of 1 at most.  The
+    mean gradient of n calls, less the exact one, is E w (or E^T x) with E's variances divided by n; its scalar product with a
+    gradient G is that of E and G w^T (x G^T): of standard deviation |G w^T| / sqrt(n) at most.  Six of those, and 2^-8 of |G|^2
+    for roundings to BF16.  (A clipped 7 is off by 1 in every call: 2 to 4 % of |G|^2.)"""
+    x, w, args, dy, matrices, mine = case(kind)
+    n = 64
+    total_x, total_w = torch.zeros(x.shape, device=DEV, dtype=torch.float64), torch.zeros(w.shape, device=DEV, dtype=torch.float64)
+    for i in range(n):
+        if "seed" in how:
+            how = dict(how, seed=how["seed"] + 1)
+        gx, gw = gradients(kind, dy, x, w, args, **how)
+        total_x += gx.double()
+        total_w += gw.double()
+    total_w = [total_w] if kind == "linear" else list(total_w)
+    for matrix, rows, got_w in zip(matrices, mine, total_w):
+        a, b, m = x[rows].double(), dy[rows].double(), matrix.double()
+        for got, want, spread in ((total_x[rows], b @ m, (b @ m) @ m.t()), (got_w, b.t() @ a, a @ (b.t() @ a).t())):
+            off = float(((got / n - want) * want).sum())
+            assert abs(off) <= 6 * float(spread.norm()) / n ** 0.5 + 2.0 ** -8 * float((want * want).sum()), off / float((want * want).sum())
+
+
+@pytest.mark.parametrize("kind", ["linear", "experts"])
+def test_gradient_rule(kind):
+    """The gradients' scale rule alone; without one a call with a seed follows the other operands' rule."""
+    x, w, args, dy, *_ = case(kind)
+    how = {rule: gradients(kind, dy, x, w, args, seed=3, gradient_rule=rule) for rule in ("floor", "ceil")}
+    for a, b, c in zip(how["floor"], gradients(kind, dy, x, w, args, seed=3), how["ceil"]):
+        assert torch.equal(a, b) and not torch.equal(a, c)
+    with pytest.raises(ValueError):
+        answer(kind, x, w, args, gradient_rule="round")
