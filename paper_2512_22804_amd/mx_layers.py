@@ -9,6 +9,8 @@ forward pass for the backward pass is kept in 4 bits, not in 16.
 """
 from __future__ import annotations
 
+import functools
+
 import torch
 
 from . import mx
@@ -55,6 +57,33 @@ def _operands(x: torch.Tensor, rows: int, cols: int, transposed: bool = True, ba
     return out, out_t
 
 
+class _NoFurther(torch.autograd.Function):
+    """Gradients as they are, whose own derivatives raise.  ``anchor`` requires a gradient, so that they do."""
+
+    @staticmethod
+    def forward(ctx, anchor, *grads):
+        return tuple(g.view_as(g) for g in grads)
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError("the 4-bit layers have first derivatives only: their gradients cannot be differentiated again")
+
+
+def _first_derivatives(backward):
+    """The kernels record no graph, so with ``create_graph`` the gradients' dependence on the inputs would be lost silently, also where ``dy``
+    does not depend on them."""
+    @functools.wraps(backward)
+    def wrapped(ctx, dy):
+        with torch.no_grad():
+            grads = backward(ctx, dy)
+        if torch.is_grad_enabled():
+            there = [g for g in grads if g is not None]
+            there = iter(_NoFurther.apply(torch.empty(0, requires_grad=True), *there))
+            grads = tuple(None if g is None else next(there) for g in grads)
+        return grads
+    return wrapped
+
+
 class _Linear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, w, scale_rule, how, training):
@@ -66,6 +95,7 @@ class _Linear(torch.autograd.Function):
         return _product(xq, wq, torch.bfloat16)
 
     @staticmethod
+    @_first_derivatives
     def backward(ctx, dy):
         xt, wt = ctx.operands
         g, gt = _operands(_bf16(dy), dy.shape[0], dy.shape[1], **ctx.how)
@@ -108,6 +138,7 @@ class _Experts(torch.autograd.Function):
         return y
 
     @staticmethod
+    @_first_derivatives
     def backward(ctx, dy):
         order, xt, wt, ys = ctx.kept
         weights, = ctx.saved_tensors

@@ -93,3 +93,20 @@ def test_gradient_rule(kind):
         assert torch.equal(a, b) and not torch.equal(a, c)
     with pytest.raises(ValueError):
         answer(kind, x, w, args, gradient_rule="round")
+
+
+@pytest.mark.parametrize("which", [0, 1, 2])
+@pytest.mark.parametrize("kind", ["linear", "experts"])
+def test_second_derivatives_raise(kind, which):
+    x, w, args, dy, *_ = case(kind)
+    inputs = [x, w, *args[1:]]
+    if which >= len(inputs):
+        which = 0
+    inputs = [t.clone().requires_grad_() for t in inputs]
+    y = answer(kind, inputs[0], inputs[1], (*args[:1], *inputs[2:]), seed=3)
+    loss = (y.float() * dy.float()).sum()
+    first, = torch.autograd.grad(loss, inputs[which], retain_graph=True)
+    g, = torch.autograd.grad(loss, inputs[which], create_graph=True)
+    assert torch.equal(g, first) and not first.requires_grad
+    with pytest.raises(RuntimeError):
+        (loss + g.square().sum()).backward()        # (without the loss there is nothing to differentiate, which raises too)
