@@ -57,6 +57,15 @@ def _operands(x: torch.Tensor, rows: int, cols: int, transposed: bool = True, ba
     return out, out_t
 
 
+def _saved(operand: mx.MxOperand | None) -> tuple:
+    """An operand as tensors for autograd to keep: hooks on saved tensors see them, and they go with the graph's buffers."""
+    return (None, None) if operand is None else (operand.codes, operand.scales)
+
+
+def _restored(codes: torch.Tensor | None, scales: torch.Tensor | None, rows: int, cols: int) -> mx.MxOperand | None:
+    return None if codes is None else mx.MxOperand(codes, scales, rows, cols)
+
+
 class _NoFurther(torch.autograd.Function):
     """Gradients as they are, whose own derivatives raise.  ``anchor`` requires a gradient, so that they do."""
 
@@ -91,13 +100,16 @@ class _Linear(torch.autograd.Function):
         # either input's transpose is what the other one's gradient reads
         xq, xt = _operands(_bf16(x), tokens, hidden, training and ctx.needs_input_grad[1], scale_rule=scale_rule)
         wq, wt = _operands(_bf16(w), w.shape[0], hidden, training and ctx.needs_input_grad[0], scale_rule=scale_rule)
-        ctx.operands, ctx.how, ctx.types = (xt, wt), how, (x.dtype, w.dtype)
+        ctx.save_for_backward(*_saved(xt), *_saved(wt))
+        ctx.sizes, ctx.how, ctx.types = (tokens, hidden, w.shape[0]), how, (x.dtype, w.dtype)
         return _product(xq, wq, torch.bfloat16)
 
     @staticmethod
     @_first_derivatives
     def backward(ctx, dy):
-        xt, wt = ctx.operands
+        tokens, hidden, width = ctx.sizes
+        kept = ctx.saved_tensors
+        xt, wt = _restored(*kept[:2], hidden, tokens), _restored(*kept[2:], hidden, width)
         g, gt = _operands(_bf16(dy), dy.shape[0], dy.shape[1], **ctx.how)
         dx = _product(g, wt, ctx.types[0]) if wt is not None else None
         dw = _product(gt, xt, ctx.types[1]) if xt is not None else None
@@ -133,15 +145,18 @@ class _Experts(torch.autograd.Function):
         y = torch.empty(tokens, width, dtype=torch.bfloat16, device=x.device)
         weights = weights.detach().contiguous()
         mx.mor_expert_combine(ys, order, weights, y)
-        ctx.save_for_backward(weights)
-        ctx.kept, ctx.how, ctx.types = (order, xt, wt, ys), how, (x.dtype, w.dtype)
+        ctx.save_for_backward(weights, order.offsets, order.slot_of, order.src, ys if ctx.needs_input_grad[3] else None, *_saved(xt), *_saved(wt))
+        ctx.sizes = (order.tokens, order.top_k, order.n_experts, order.align, order.capacity), hidden, width
+        ctx.how, ctx.types = how, (x.dtype, w.dtype)
         return y
 
     @staticmethod
     @_first_derivatives
     def backward(ctx, dy):
-        order, xt, wt, ys = ctx.kept
-        weights, = ctx.saved_tensors
+        sizes, hidden, width = ctx.sizes
+        weights, offsets, slot_of, src, ys, *kept = ctx.saved_tensors
+        order = mx.ExpertOrder(*sizes, offsets, slot_of, src, None)
+        xt, wt = _restored(*kept[:2], hidden, order.capacity), _restored(*kept[2:], hidden, width)
         dy = _bf16(dy)
         dx = dw = dweights = None
         if xt is not None or wt is not None:

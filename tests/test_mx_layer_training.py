@@ -110,3 +110,26 @@ def test_second_derivatives_raise(kind, which):
     assert torch.equal(g, first) and not first.requires_grad
     with pytest.raises(RuntimeError):
         (loss + g.square().sum()).backward()        # (without the loss there is nothing to differentiate, which raises too)
+
+
+@pytest.mark.parametrize("kind", ["linear", "experts"])
+def test_kept_operands_are_saved_tensors(kind):
+    """Hooks on saved tensors see the operands that the backward pass reads, may keep them elsewhere, and the graph lets go of them."""
+    x, w, args, dy, *_ = case(kind)
+    want = gradients(kind, dy, x, w, args, seed=3)
+    sizes = []
+
+    def pack(t):
+        sizes.append(t.numel() * t.element_size())
+        return t.cpu()
+
+    a, b = x.clone().requires_grad_(), w.clone().requires_grad_()
+    with torch.autograd.graph.saved_tensors_hooks(pack, lambda t: t.to(DEV)):
+        y = answer(kind, a, b, args, seed=3)
+    assert sum(sizes) >= (x.numel() + w.numel()) * 17 // 32                     # both transposes
+    y.backward(dy, retain_graph=True)
+    assert torch.equal(a.grad, want[0]) and torch.equal(b.grad, want[1])
+    y.backward(dy)
+    assert torch.equal(a.grad, 2 * want[0]) and torch.equal(b.grad, 2 * want[1])
+    with pytest.raises(RuntimeError):
+        y.backward(dy)
