@@ -49,9 +49,9 @@ def _product(a: mx.MxOperand, b: mx.MxOperand, dtype: torch.dtype) -> torch.Tens
     return c
 
 
-def _operands(x: torch.Tensor, rows: int, cols: int, transposed: bool = True, batch: int | None = None, **how):
-    """``x`` as an operand of ``rows`` x ``cols`` and, if wanted, its transpose."""
-    out = mx.alloc_operand(rows, cols, x.device, batch)
+def _operands(x: torch.Tensor, rows: int, cols: int, transposed: bool = True, batch: int | None = None, plain: bool = True, **how):
+    """``x`` as an operand of ``rows`` x ``cols`` and its transpose, None for what is not wanted."""
+    out = mx.alloc_operand(rows, cols, x.device, batch) if plain else None
     out_t = mx.alloc_operand(cols, rows, x.device, batch) if transposed else None
     mx.mor_mx_quantize(x, out, out_t, **how)
     return out, out_t
@@ -110,7 +110,7 @@ class _Linear(torch.autograd.Function):
         tokens, hidden, width = ctx.sizes
         kept = ctx.saved_tensors
         xt, wt = _restored(*kept[:2], hidden, tokens), _restored(*kept[2:], hidden, width)
-        g, gt = _operands(_bf16(dy), dy.shape[0], dy.shape[1], **ctx.how)
+        g, gt = _operands(_bf16(dy), dy.shape[0], dy.shape[1], xt is not None, plain=wt is not None, **ctx.how)
         dx = _product(g, wt, ctx.types[0]) if wt is not None else None
         dw = _product(gt, xt, ctx.types[1]) if xt is not None else None
         return dx, dw, None, None, None
@@ -161,7 +161,7 @@ class _Experts(torch.autograd.Function):
         dx = dw = dweights = None
         if xt is not None or wt is not None:
             # the rows' gradients, each times its choice's weight, go from the tokens' straight into 4 bits
-            g, gt = _operands(dy, order.capacity, dy.shape[1], xt is not None, order=order, weights=weights, **ctx.how)
+            g, gt = _operands(dy, order.capacity, dy.shape[1], xt is not None, plain=wt is not None, order=order, weights=weights, **ctx.how)
         if wt is not None:
             dxs = torch.empty(order.capacity, wt.rows, dtype=torch.bfloat16, device=dy.device)
             mx.mor_mx_product_rows(g, wt, order, dxs)

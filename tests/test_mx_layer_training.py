@@ -133,3 +133,26 @@ def test_kept_operands_are_saved_tensors(kind):
     assert torch.equal(a.grad, 2 * want[0]) and torch.equal(b.grad, 2 * want[1])
     with pytest.raises(RuntimeError):
         y.backward(dy)
+
+
+@pytest.mark.parametrize("kind", ["linear", "experts"])
+def test_forms_that_nothing_reads_are_not_made(kind, monkeypatch):
+    """dy as it is for the tokens' gradient, transposed for the weights', and nothing for the routing weights' alone."""
+    x, w, args, dy, *_ = case(kind)
+    made = []
+    quantize = mx.mor_mx_quantize
+
+    def note(x, out=None, out_t=None, **how):
+        made.append((out is not None, out_t is not None))
+        quantize(x, out, out_t, **how)
+
+    for need_x, need_w in ((True, True), (True, False), (False, True), (False, False)):
+        a, b = x.clone().requires_grad_(need_x), w.clone().requires_grad_(need_w)
+        router = [t.clone().requires_grad_() if t.is_floating_point() else t for t in args]
+        y = answer(kind, a, b, router, seed=3)
+        if y.requires_grad:
+            with monkeypatch.context() as m:
+                m.setattr(mx, "mor_mx_quantize", note)
+                made.clear()
+                y.backward(dy)
+            assert made == ([(need_x, need_w)] if need_x or need_w else [])
