@@ -29,6 +29,12 @@ def _check(x: torch.Tensor, w: torch.Tensor, dims: int) -> None:
         raise ValueError(f"shapes do not match: x {tuple(x.shape)}, w {tuple(w.shape)}")
 
 
+def _check_choices(x: torch.Tensor, ids: torch.Tensor, weights: torch.Tensor) -> None:
+    # (weights one after the other, in the choices' order, are as good; of another shape they would be another choice's)
+    if ids.dim() != 2 or ids.shape[0] != x.shape[0] or weights.shape not in (ids.shape, (ids.numel(),)):
+        raise ValueError(f"shapes do not match: x {tuple(x.shape)}, ids {tuple(ids.shape)}, weights {tuple(weights.shape)}")
+
+
 def _gradients(scale_rule: str, seed: int | None, gradient_rule: str | None, rounds: bool) -> dict:
     """How a call's gradients are rounded.  Without a seed of the caller's it is a new one, if there is a gradient to round at all."""
     if gradient_rule is None:
@@ -183,6 +189,7 @@ def experts(x: torch.Tensor, w: torch.Tensor, ids: torch.Tensor, weights: torch.
     the token's row of ``x`` (tokens, hidden) times that expert's matrix of ``w`` (experts, width, hidden), transposed; in BF16.  ``seed``
     and ``gradient_rule`` as for :func:`linear`."""
     _check(x, w, 3)
+    _check_choices(x, ids, weights)
     training = torch.is_grad_enabled()
     how = _gradients(scale_rule, seed, gradient_rule, training and (x.requires_grad or w.requires_grad))
     return _Experts.apply(x, w, ids, weights, scale_rule, how, training)
@@ -192,10 +199,15 @@ class ServedExperts:
     """The experts' matrices in 4 bits, for tokens as they come: no gradient, segments as short as the tokens make them."""
 
     def __init__(self, w: torch.Tensor, scale_rule: str = "floor"):
+        if w.dim() != 3:
+            raise ValueError(f"w must be (experts, width, hidden), not {tuple(w.shape)}")
         self.scale_rule = scale_rule
         self.w, _ = _operands(_bf16(w), w.shape[1], w.shape[2], False, w.shape[0], scale_rule=scale_rule)
 
     def __call__(self, x: torch.Tensor, ids: torch.Tensor, weights: torch.Tensor) -> torch.Tensor:
+        if x.dim() != 2 or x.shape[1] != self.w.cols:
+            raise ValueError(f"x must be (tokens, {self.w.cols}), not {tuple(x.shape)}")
+        _check_choices(x, ids, weights)
         tokens, hidden = x.shape
         order = mx.alloc_order(tokens, ids.shape[1], self.w.batch, x.device, align=1)
         mx.mor_expert_sort(ids, order)
