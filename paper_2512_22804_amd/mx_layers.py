@@ -192,7 +192,7 @@ def experts(x: torch.Tensor, w: torch.Tensor, ids: torch.Tensor, weights: torch.
     _check_choices(x, ids, weights)
     training = torch.is_grad_enabled()
     how = _gradients(scale_rule, seed, gradient_rule, training and (x.requires_grad or w.requires_grad))
-    return _Experts.apply(x, w, ids, weights, scale_rule, how, training)
+    return _Experts.apply(x, w, ids.contiguous(), weights, scale_rule, how, training)
 
 
 class ServedExperts:
@@ -210,12 +210,12 @@ class ServedExperts:
         _check_choices(x, ids, weights)
         tokens, hidden = x.shape
         order = mx.alloc_order(tokens, ids.shape[1], self.w.batch, x.device, align=1)
-        mx.mor_expert_sort(ids, order)
+        mx.mor_expert_sort(ids.contiguous(), order)
         xq, _ = _operands(_bf16(x), order.capacity, hidden, False, scale_rule=self.scale_rule, order=order)
         ys = torch.empty(order.capacity, self.w.rows, dtype=torch.bfloat16, device=x.device)
         mx.mor_mx_product_rows(xq, self.w, order, ys)
         y = torch.empty(tokens, self.w.rows, dtype=torch.bfloat16, device=x.device)
-        mx.mor_expert_combine(ys, order, weights, y)
+        mx.mor_expert_combine(ys, order, weights.contiguous(), y)
         return y
 
 

@@ -23,3 +23,15 @@ def test_layers_of_experts_look_at_shapes():
                 call(*wrong)
     with pytest.raises(ValueError):
         mx_layers.ServedExperts(w[0])
+
+
+@pytest.mark.gpu
+def test_layers_of_experts_take_any_strides():
+    """A router's tensors as they come: a part of its columns, or its rows side by side."""
+    x, w = torch.randn(6, 64, device=DEV), torch.randn(3, 40, 64, device=DEV)
+    ids, weights = torch.randint(0, 3, (6, 4), dtype=torch.int32, device=DEV), torch.rand(6, 4, device=DEV)
+    served = mx_layers.ServedExperts(w)
+    for call in (lambda *a: mx_layers.experts(a[0], w, *a[1:]), served):
+        want = call(x, ids[:, :2].contiguous(), weights[:, :2].contiguous())
+        assert torch.equal(call(x, ids[:, :2], weights[:, :2]), want)
+        assert torch.equal(call(x, ids[:, :2].t().contiguous().t(), weights[:, :2].t().contiguous().t()), want)
