@@ -138,11 +138,12 @@ class MxOperand:
             raise ValueError("codes and scales must have the same batch and rows")
         if self.codes.device != self.scales.device:
             raise ValueError("codes and scales must live on one device")
+        # a lone row's distance to the next can be anything; the bytes that its blocks take serve
         lone = self.rows == 1
         object.__setattr__(self, "batch", self.codes.shape[0] if self.codes.dim() == 3 else 1)
         object.__setattr__(self, "_index", self.codes.get_device())
         object.__setattr__(self, "_struct", MorMxOperand(
-            None, self.codes.shape[-1] if lone else self.codes.stride(-2), None, self.scales.shape[-1] if lone else self.scales.stride(-2),
+            None, 16 * self.blocks if lone else self.codes.stride(-2), None, -(-self.blocks // 4) * 4 if lone else self.scales.stride(-2),
             self.codes.stride(0) if self.codes.dim() == 3 else 0, self.scales.stride(0) if self.scales.dim() == 3 else 0))
 
     @property

@@ -35,3 +35,28 @@ def test_layers_of_experts_take_any_strides():
         want = call(x, ids[:, :2].contiguous(), weights[:, :2].contiguous())
         assert torch.equal(call(x, ids[:, :2], weights[:, :2]), want)
         assert torch.equal(call(x, ids[:, :2].t().contiguous().t(), weights[:, :2].t().contiguous().t()), want)
+
+
+def test_an_operand_of_one_row_cut_out_of_a_larger_one():
+    """Its row's distance to the next is nobody's: what counts are the bytes that its blocks take."""
+    codes, scales = torch.zeros(4, 64, dtype=torch.uint8), torch.zeros(4, 8, dtype=torch.uint8)
+    for cut in (slice(0, 1), slice(2, 3)):
+        op = mx.MxOperand(codes[cut, :56], scales[cut, :3], 1, 96)
+        assert op._struct.ld_codes % 16 == 0 and op._struct.ld_codes >= 48
+        assert op._struct.ld_scales % 4 == 0 and op._struct.ld_scales >= 3
+
+
+@pytest.mark.gpu
+def test_an_operand_of_one_row_cut_out_of_a_larger_one_is_written_and_read():
+    x = torch.randn(1, 96, device=DEV).to(torch.bfloat16)
+    want, y = mx.alloc_operand(1, 96, DEV), torch.empty(1, 96, device=DEV, dtype=torch.bfloat16)
+    mx.mor_mx_quantize(x, want)
+    codes, scales = torch.full((4, 64), 0xA5, dtype=torch.uint8, device=DEV), torch.full((4, 8), 0xA5, dtype=torch.uint8, device=DEV)
+    op = mx.MxOperand(codes[1:2, :56], scales[1:2, :3], 1, 96)
+    mx.mor_mx_quantize(x, op)
+    assert torch.equal(codes[1:2, :48], want.codes) and torch.equal(scales[1:2, :3], want.scales[:, :3])
+    assert (codes[[0, 2, 3]] == 0xA5).all() and (scales[[0, 2, 3]] == 0xA5).all() and (codes[1, 48:] == 0xA5).all() and (scales[1, 4:] == 0xA5).all()
+    mx.mor_mx_dequantize(op, y)
+    back = torch.empty_like(y)
+    mx.mor_mx_dequantize(want, back)
+    assert torch.equal(y, back)
