@@ -86,7 +86,7 @@ mor_status mor_mx_quantize(const mor_mx_params* p, const uint16_t* x, const mor_
         rows = order->capacity;
     } else if (weights) return MOR_ERR_UNSUPPORTED;
     if (rows == 0) return MOR_OK;
-    if ((st = check_matrix(x, p->ld, p->cols)) != MOR_OK) return st;
+    if (p->rows > 0 && (st = check_matrix(x, p->ld, p->cols)) != MOR_OK) return st;    // (slots without tokens: x has no address)
     if (!aligned(weights, 4)) return MOR_ERR_ALIGN;
     if (out && (st = check_operand(out, p->cols, batched)) != MOR_OK) return st;
     if (out_t && (st = check_operand(out_t, rows, batched)) != MOR_OK) return st;

@@ -60,3 +60,34 @@ def test_an_operand_of_one_row_cut_out_of_a_larger_one_is_written_and_read():
     back = torch.empty_like(y)
     mx.mor_mx_dequantize(want, back)
     assert torch.equal(y, back)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("how", ["rows", "both", "stochastic"])
+def test_slots_without_tokens_are_quantised(how):
+    """An order of fixed capacity and no tokens: x has no address, every slot holds zeros."""
+    capacity, d = 256, 64
+    ints = lambda n: torch.empty(n, dtype=torch.int32, device=DEV)
+    order = mx.ExpertOrder(0, 2, 3, 128, capacity, ints(4), ints(0), ints(capacity), None)
+    mx.mor_expert_sort(ints(0).view(0, 2), order)
+    out = mx.alloc_operand(capacity, d, DEV)
+    out_t = mx.alloc_operand(d, capacity, DEV) if how != "rows" else None
+    for op in (out, out_t):
+        if op is not None:
+            op.codes.fill_(0xA5)
+    mx.mor_mx_quantize(torch.empty(0, d, dtype=torch.bfloat16, device=DEV), out, out_t, order=order,
+                       rounding="stochastic" if how == "stochastic" else "nearest")
+    assert all((op.codes == 0).all() and (op.scales[:, :op.blocks] == 127).all() for op in (out, out_t) if op is not None)
+
+
+def test_slots_without_tokens_need_no_tokens_address():
+    """(No kernel is launched: what is refused is the operand, looked at behind x.)"""
+    at = 1 << 40
+    order = mx.MorExpertOrder(0, 2, 3, 128, 128, 0, at, None, at)
+    params = mx.MorMxParams(0, 32, 32, 1, 0, 0, 0, 0)
+    out = mx.MorMxOperand(at + 8, 16, at, 4, 0, 0)
+    assert mx.load().mor_mx_quantize(C.byref(params), None, C.byref(out), None, C.byref(order), None, None) == 3
+    order.tokens = params.rows = 1
+    order.slot_of = at
+    order.capacity = 256
+    assert mx.load().mor_mx_quantize(C.byref(params), None, C.byref(out), None, C.byref(order), None, None) == 1
