@@ -73,24 +73,19 @@ def load():
 
 def _device(where: str, *things) -> int:
     """Index of the device that all of ``things`` (tensors, operands, orders; None: not there) live on."""
-    device = None
-    for t in things:
-        if t is not None:
-            index = t.get_device()
-            if index < 0:
-                raise ValueError(f"{where}: all tensors must live in device memory")
-            if index != device:
-                if device is not None:
-                    raise ValueError(f"{where}: tensors on devices {device} and {index}")
-                device = index
-    return device
+    found = {t.get_device() for t in things if t is not None}
+    if min(found) < 0:
+        raise ValueError(f"{where}: all tensors must live in device memory")
+    if len(found) > 1:
+        raise ValueError(f"{where}: tensors on devices {sorted(found)}")
+    return found.pop()
 
 
 def _run(where: str, device: int, *args) -> None:
     """Calls the library with ``device`` as the current one and its current stream."""
-    call = getattr(load(), where)
+    call = getattr(_lib or load(), where)
     if device == torch.cuda.current_device():
-        rc = call(*args, binding._stream())
+        rc = call(*args, binding._raw_stream(device) if binding._raw_stream is not None else binding._stream())
     else:
         with torch.cuda.device(device):
             rc = call(*args, binding._stream())
@@ -100,8 +95,6 @@ def _run(where: str, device: int, *args) -> None:
 
 def _matrix(t: torch.Tensor, name: str, types=(torch.bfloat16, torch.int16)) -> int:
     """Checks a matrix (or a batch of them) and returns the elements between its rows."""
-    if not t.is_cuda:
-        raise ValueError(f"{name} must live in device memory")
     if t.dtype not in types:
         raise ValueError(f"{name}: {t.dtype} is not one of {types}")
     shape, stride = t.shape, t.stride()
@@ -118,8 +111,8 @@ def _batch(t: torch.Tensor) -> tuple[int, int]:
 def _vector(t: torch.Tensor | None, name: str, dtype, n: int) -> None:
     if t is None:
         return
-    if not t.is_cuda or t.dtype != dtype or t.numel() != n or not t.is_contiguous():
-        raise ValueError(f"{name} must be {n} contiguous elements of {dtype} in device memory")
+    if t.dtype != dtype or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name} must be {n} contiguous elements of {dtype}")
 
 
 @dataclass(frozen=True)
@@ -141,7 +134,7 @@ class MxOperand:
         # a lone row's distance to the next can be anything; the bytes that its blocks take serve
         lone = self.rows == 1
         object.__setattr__(self, "batch", self.codes.shape[0] if self.codes.dim() == 3 else 1)
-        object.__setattr__(self, "_index", self.codes.get_device())
+        object.__setattr__(self, "_index", self.codes.get_device())         # (its buffers do not change)
         object.__setattr__(self, "_struct", MorMxOperand(
             None, 16 * self.blocks if lone else self.codes.stride(-2), None, -(-self.blocks // 4) * 4 if lone else self.scales.stride(-2),
             self.codes.stride(0) if self.codes.dim() == 3 else 0, self.scales.stride(0) if self.scales.dim() == 3 else 0))
@@ -229,7 +222,11 @@ def mor_mx_quantize(x: torch.Tensor, out: MxOperand | None = None, out_t: MxOper
         if operand is not None and ((operand.rows, operand.cols) != shape or operand.batch != batch):
             raise ValueError(f"{name} must be {batch} operand(s) of {shape[0]} x {shape[1]}")
     params = MorMxParams(rows, cols, ld, batch, batch_x, SCALE_RULE[scale_rule], ROUNDING[rounding], seed & 0xFFFFFFFFFFFFFFFF)
-    _run("mor_mx_quantize", _device("mor_mx_quantize", x, out, out_t, order, weights), C.addressof(params), x.data_ptr(),
+    device = x.get_device()
+    if device < 0 or (out is not None and out._index != device) or (out_t is not None and out_t._index != device) or \
+            (order is not None and order._index != device) or (weights is not None and weights.get_device() != device):
+        _device("mor_mx_quantize", x, out, out_t, order, weights)
+    _run("mor_mx_quantize", device, C.addressof(params), x.data_ptr(),
          out.struct() if out is not None else None, out_t.struct() if out_t is not None else None,
          order.struct() if order is not None else None, binding._ptr(weights))
 
@@ -240,7 +237,10 @@ def mor_mx_dequantize(operand: MxOperand, y: torch.Tensor) -> None:
     batch, batch_y = _batch(y)
     if y.shape[-2:] != (operand.rows, operand.cols) or batch != operand.batch:
         raise ValueError(f"y must be {operand.batch} matrices of {operand.rows} x {operand.cols}")
-    _run("mor_mx_dequantize", _device("mor_mx_dequantize", operand, y), operand.rows, operand.cols, batch, operand.struct(),
+    device = operand._index
+    if device < 0 or y.get_device() != device:
+        _device("mor_mx_dequantize", operand, y)
+    _run("mor_mx_dequantize", device, operand.rows, operand.cols, batch, operand.struct(),
          y.data_ptr(), ld, batch_y)
 
 
@@ -262,7 +262,10 @@ def mor_mx_product(a: MxOperand, b: MxOperand, c: torch.Tensor, workspace: torch
     ld = _matrix(c, "c", _OUT)
     if a.cols != b.cols or a.batch != 1 or b.batch != 1 or c.shape != (a.rows, b.rows):
         raise ValueError(f"shapes do not match: {a.rows} x {a.cols}, {b.rows} x {b.cols}, result {tuple(c.shape)}")
-    _run("mor_mx_product", _device("mor_mx_product", a, b, c, workspace), a.rows, b.rows, a.cols, a.struct(), b.struct(), c.data_ptr(), ld,
+    device = a._index
+    if device < 0 or b._index != device or c.get_device() != device or (workspace is not None and workspace.get_device() != device):
+        _device("mor_mx_product", a, b, c, workspace)
+    _run("mor_mx_product", device, a.rows, b.rows, a.cols, a.struct(), b.struct(), c.data_ptr(), ld,
          _OUT[c.dtype], binding._ptr(workspace), workspace.numel() if workspace is not None else 0)
 
 
@@ -272,7 +275,10 @@ def mor_mx_product_rows(a: MxOperand, b: MxOperand, order: ExpertOrder, c: torch
     if a.cols != b.cols or a.batch != 1 or a.rows != order.capacity or b.batch != order.n_experts or c.shape != (a.rows, b.rows):
         raise ValueError(f"shapes do not match: {a.rows} x {a.cols}, {b.batch} of {b.rows} x {b.cols}, {order.n_experts} experts, "
                          f"{order.capacity} slots, result {tuple(c.shape)}")
-    _run("mor_mx_product_rows", _device("mor_mx_product_rows", a, b, order, c), b.rows, a.cols, a.struct(), b.struct(), order.struct(),
+    device = a._index
+    if device < 0 or b._index != device or order._index != device or c.get_device() != device:
+        _device("mor_mx_product_rows", a, b, order, c)
+    _run("mor_mx_product_rows", device, b.rows, a.cols, a.struct(), b.struct(), order.struct(),
          c.data_ptr(), ld, _OUT[c.dtype])
 
 
@@ -283,7 +289,10 @@ def mor_mx_product_depth(a: MxOperand, b: MxOperand, order: ExpertOrder, c: torc
             c.dim() != 3 or c.shape != (order.n_experts, a.rows, b.rows):
         raise ValueError(f"shapes do not match: {a.rows} x {a.cols}, {b.rows} x {b.cols}, {order.n_experts} experts, "
                          f"{order.capacity} slots, result {tuple(c.shape)}")
-    _run("mor_mx_product_depth", _device("mor_mx_product_depth", a, b, order, c), a.rows, b.rows, a.struct(), b.struct(), order.struct(),
+    device = a._index
+    if device < 0 or b._index != device or order._index != device or c.get_device() != device:
+        _device("mor_mx_product_depth", a, b, order, c)
+    _run("mor_mx_product_depth", device, a.rows, b.rows, a.struct(), b.struct(), order.struct(),
          c.data_ptr(), ld, _batch(c)[1], _OUT[c.dtype])
 
 
@@ -291,7 +300,10 @@ def mor_expert_sort(ids: torch.Tensor, order: ExpertOrder) -> None:
     """``ids`` (tokens, top_k) int32: the expert of each choice; outside [0, n_experts): dropped."""
     _vector(ids, "ids", torch.int32, order.tokens * order.top_k)
     ws = order.workspace
-    _run("mor_expert_sort", _device("mor_expert_sort", ids, order), ids.data_ptr(), order.struct(), binding._ptr(ws),
+    device = order._index
+    if ids.get_device() != device:
+        _device("mor_expert_sort", ids, order)
+    _run("mor_expert_sort", device, ids.data_ptr(), order.struct(), binding._ptr(ws),
          ws.numel() if ws is not None else 0)
 
 
@@ -308,7 +320,10 @@ def mor_expert_gather(x: torch.Tensor, order: ExpertOrder, xs: torch.Tensor) -> 
     """``xs`` (capacity, d): the token's row for every slot, zeros for empty ones."""
     d = x.shape[-1]
     ld_x, ld_xs = _rows(x, "x", order.tokens, d), _rows(xs, "xs", order.capacity, d)
-    _run("mor_expert_gather", _device("mor_expert_gather", x, order, xs), x.data_ptr(), ld_x, d, order.struct(), xs.data_ptr(), ld_xs)
+    device = order._index
+    if x.get_device() != device or xs.get_device() != device:
+        _device("mor_expert_gather", x, order, xs)
+    _run("mor_expert_gather", device, x.data_ptr(), ld_x, d, order.struct(), xs.data_ptr(), ld_xs)
 
 
 def mor_expert_combine(ys: torch.Tensor, order: ExpertOrder, weights: torch.Tensor | None, y: torch.Tensor) -> None:
@@ -316,8 +331,10 @@ def mor_expert_combine(ys: torch.Tensor, order: ExpertOrder, weights: torch.Tens
     d = ys.shape[-1]
     ld_ys, ld_y = _rows(ys, "ys", order.capacity, d), _rows(y, "y", order.tokens, d)
     _vector(weights, "weights", torch.float32, order.tokens * order.top_k)
-    _run("mor_expert_combine", _device("mor_expert_combine", ys, order, weights, y), ys.data_ptr(), ld_ys, d, order.struct(),
-         binding._ptr(weights), y.data_ptr(), ld_y)
+    device = order._index
+    if ys.get_device() != device or y.get_device() != device or (weights is not None and weights.get_device() != device):
+        _device("mor_expert_combine", ys, order, weights, y)
+    _run("mor_expert_combine", device, ys.data_ptr(), ld_ys, d, order.struct(), binding._ptr(weights), y.data_ptr(), ld_y)
 
 
 def mor_expert_combine_backward(dy: torch.Tensor, ys: torch.Tensor | None, order: ExpertOrder, weights: torch.Tensor | None,
@@ -327,5 +344,6 @@ def mor_expert_combine_backward(dy: torch.Tensor, ys: torch.Tensor | None, order
     ld_dy, ld_ys, ld_dys = _rows(dy, "dy", order.tokens, d), _rows(ys, "ys", order.capacity, d), _rows(dys, "dys", order.capacity, d)
     _vector(weights, "weights", torch.float32, order.tokens * order.top_k)
     _vector(dweights, "dweights", torch.float32, order.tokens * order.top_k)
-    _run("mor_expert_combine_backward", _device("mor_expert_combine_backward", dy, ys, order, weights, dys, dweights), dy.data_ptr(), ld_dy,
-         binding._ptr(ys), ld_ys, d, order.struct(), binding._ptr(weights), binding._ptr(dys), ld_dys, binding._ptr(dweights))
+    device = _device("mor_expert_combine_backward", dy, ys, order, weights, dys, dweights)
+    _run("mor_expert_combine_backward", device, dy.data_ptr(), ld_dy, binding._ptr(ys), ld_ys, d, order.struct(), binding._ptr(weights),
+         binding._ptr(dys), ld_dys, binding._ptr(dweights))
