@@ -137,12 +137,20 @@ mor_status mor_expert_gather(const uint16_t* x, int64_t ld_x, int64_t d, const m
 mor_status mor_expert_combine(const uint16_t* ys, int64_t ld_ys, int64_t d, const mor_expert_order* order, const float* weights,
                               uint16_t* y, int64_t ld_y, void* stream);
 
+/* The same of rows in binary32, as mor_mx_product_rows writes them too: no rounding between the product and the sum.  y: BF16 or binary32. */
+mor_status mor_expert_combine_f32(const float* ys, int64_t ld_ys, int64_t d, const mor_expert_order* order, const float* weights, void* y,
+                                  int64_t ld_y, int32_t y_type, void* stream);
+
 /* The gradients of mor_expert_combine with weights: dys [capacity x d] = weights[choice] * dy[its token] (zeros in empty slots) and
  * dweights [tokens x top_k] = <dy[t], ys[slot]> in binary32 (0 for a dropped choice).  Either may be NULL; ys is read for
  * dweights only, weights for dys only. */
 mor_status mor_expert_combine_backward(const uint16_t* dy, int64_t ld_dy, const uint16_t* ys, int64_t ld_ys, int64_t d,
                                        const mor_expert_order* order, const float* weights, uint16_t* dys, int64_t ld_dys,
                                        float* dweights, void* stream);
+/* The same of rows ys in binary32; dys stays BF16. */
+mor_status mor_expert_combine_backward_f32(const uint16_t* dy, int64_t ld_dy, const float* ys, int64_t ld_ys, int64_t d,
+                                           const mor_expert_order* order, const float* weights, uint16_t* dys, int64_t ld_dys,
+                                           float* dweights, void* stream);
 
 #ifdef __cplusplus
 }

@@ -40,6 +40,30 @@ mor_status check_order(const mor_expert_order* o) {
     if (!aligned(o->offsets, 4) || !aligned(o->slot_of, 4) || !aligned(o->src, 4)) return MOR_ERR_ALIGN;
     return MOR_OK;
 }
+mor_status check_combine(const void* ys, int64_t ld_ys, int ys_size, int64_t d, const mor_expert_order* order, const float* weights, const void* y,
+                         int64_t ld_y, int y_size) {
+    mor_status st = check_order(order);
+    if (st != MOR_OK) return st;
+    if (d < 1 || d > kMaxDim) return MOR_ERR_SHAPE;
+    if (order->tokens == 0) return MOR_OK;
+    if ((st = check_matrix(ys, ld_ys, d, ys_size)) != MOR_OK || (st = check_matrix(y, ld_y, d, y_size)) != MOR_OK) return st;
+    return aligned(weights, 4) ? MOR_OK : MOR_ERR_ALIGN;
+}
+mor_status check_combine_backward(const uint16_t* dy, int64_t ld_dy, const void* ys, int64_t ld_ys, int ys_size, int64_t d,
+                                  const mor_expert_order* order, const float* weights, const uint16_t* dys, int64_t ld_dys, const float* dweights) {
+    mor_status st = check_order(order);
+    if (st != MOR_OK) return st;
+    if (d < 1 || d > kMaxDim) return MOR_ERR_SHAPE;
+    if (order->capacity == 0) return MOR_OK;            // empty gradients have no address
+    if (!dys && !dweights) return MOR_ERR_NULL;
+    if (order->tokens > 0) {
+        if ((st = check_matrix(dy, ld_dy, d)) != MOR_OK) return st;
+        if (dweights && (st = check_matrix(ys, ld_ys, d, ys_size)) != MOR_OK) return st;
+        if (dys && !weights) return MOR_ERR_NULL;
+    }
+    if (dys && (st = check_matrix(dys, ld_dys, d)) != MOR_OK) return st;
+    return aligned(weights, 4) && aligned(dweights, 4) ? MOR_OK : MOR_ERR_ALIGN;
+}
 mor::MxOrder order_of(const mor_expert_order* o) {
     return mor::MxOrder{o->tokens, o->top_k, o->n_experts, o->align, o->capacity, o->offsets, o->slot_of, o->src};
 }
@@ -211,31 +235,34 @@ mor_status mor_expert_gather(const uint16_t* x, int64_t ld_x, int64_t d, const m
 
 mor_status mor_expert_combine(const uint16_t* ys, int64_t ld_ys, int64_t d, const mor_expert_order* order, const float* weights,
                               uint16_t* y, int64_t ld_y, void* stream) {
-    mor_status st = check_order(order);
-    if (st != MOR_OK) return st;
-    if (d < 1 || d > kMaxDim) return MOR_ERR_SHAPE;
-    if (order->tokens == 0) return MOR_OK;
-    if ((st = check_matrix(ys, ld_ys, d)) != MOR_OK || (st = check_matrix(y, ld_y, d)) != MOR_OK) return st;
-    if (!aligned(weights, 4)) return MOR_ERR_ALIGN;
+    const mor_status st = check_combine(ys, ld_ys, 2, d, order, weights, y, ld_y, 2);
+    if (st != MOR_OK || order->tokens == 0) return st;
     return launched(mor::launch_expert_combine(ys, ld_ys, d, order_of(order), weights, y, ld_y, (hipStream_t)stream));
+}
+
+mor_status mor_expert_combine_f32(const float* ys, int64_t ld_ys, int64_t d, const mor_expert_order* order, const float* weights, void* y,
+                                  int64_t ld_y, int32_t y_type, void* stream) {
+    if (y_type != MOR_MX_OUT_BF16 && y_type != MOR_MX_OUT_F32) return MOR_ERR_UNSUPPORTED;
+    const bool y_f32 = y_type == MOR_MX_OUT_F32;
+    const mor_status st = check_combine(ys, ld_ys, 4, d, order, weights, y, ld_y, y_f32 ? 4 : 2);
+    if (st != MOR_OK || order->tokens == 0) return st;
+    return launched(mor::launch_expert_combine_f32(ys, ld_ys, d, order_of(order), weights, y, ld_y, y_f32, (hipStream_t)stream));
 }
 
 mor_status mor_expert_combine_backward(const uint16_t* dy, int64_t ld_dy, const uint16_t* ys, int64_t ld_ys, int64_t d,
                                        const mor_expert_order* order, const float* weights, uint16_t* dys, int64_t ld_dys,
                                        float* dweights, void* stream) {
-    mor_status st = check_order(order);
-    if (st != MOR_OK) return st;
-    if (d < 1 || d > kMaxDim) return MOR_ERR_SHAPE;
-    if (order->capacity == 0) return MOR_OK;            // empty gradients have no address
-    if (!dys && !dweights) return MOR_ERR_NULL;
-    if (order->tokens > 0) {
-        if ((st = check_matrix(dy, ld_dy, d)) != MOR_OK) return st;
-        if (dweights && (st = check_matrix(ys, ld_ys, d)) != MOR_OK) return st;
-        if (dys && !weights) return MOR_ERR_NULL;
-    }
-    if (dys && (st = check_matrix(dys, ld_dys, d)) != MOR_OK) return st;
-    if (!aligned(weights, 4) || !aligned(dweights, 4)) return MOR_ERR_ALIGN;
+    const mor_status st = check_combine_backward(dy, ld_dy, ys, ld_ys, 2, d, order, weights, dys, ld_dys, dweights);
+    if (st != MOR_OK || order->capacity == 0) return st;
     return launched(mor::launch_expert_combine_backward(dy, ld_dy, ys, ld_ys, d, order_of(order), weights, dys, ld_dys, dweights, (hipStream_t)stream));
+}
+
+mor_status mor_expert_combine_backward_f32(const uint16_t* dy, int64_t ld_dy, const float* ys, int64_t ld_ys, int64_t d,
+                                           const mor_expert_order* order, const float* weights, uint16_t* dys, int64_t ld_dys,
+                                           float* dweights, void* stream) {
+    const mor_status st = check_combine_backward(dy, ld_dy, ys, ld_ys, 4, d, order, weights, dys, ld_dys, dweights);
+    if (st != MOR_OK || order->capacity == 0) return st;
+    return launched(mor::launch_expert_combine_backward_f32(dy, ld_dy, ys, ld_ys, d, order_of(order), weights, dys, ld_dys, dweights, (hipStream_t)stream));
 }
 
 }  // extern "C"

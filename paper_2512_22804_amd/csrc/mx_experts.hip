@@ -168,12 +168,62 @@ __global__ __launch_bounds__(256) void k_expert_gather(const uint16_t* x, int64_
     }
 }
 
+// Eight elements of a row from column c on as they are in memory, BF16 or binary32, and their values.  Loading and using are apart, so
+// that several rows can be on their way.
+template <class T, bool STREAM>
+struct Piece;
+template <bool STREAM>
+struct Piece<uint16_t, STREAM> {
+    u32x4 raw;
+    __device__ __forceinline__ void load(const uint16_t* row, int64_t c, int64_t d) { raw = load8_start<STREAM>(row, c, d); }
+    __device__ __forceinline__ void clear() { raw = u32x4{0u, 0u, 0u, 0u}; }
+    __device__ __forceinline__ void values(int64_t c, int64_t d, float (&f)[8]) const { widen8(c < d ? load8_end(raw, c, d) : raw, f); }
+};
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef f32x4 f32x4_anywhere __attribute__((aligned(4)));
+template <bool STREAM>
+struct Piece<float, STREAM> {
+    f32x4 raw[2];
+    __device__ __forceinline__ void load(const float* row, int64_t c, int64_t d) {
+        const f32x4_anywhere* p = reinterpret_cast<const f32x4_anywhere*>(row + c);
+        if (c + 8 <= d) {
+            raw[0] = STREAM ? __builtin_nontemporal_load(p) : p[0];
+            raw[1] = STREAM ? __builtin_nontemporal_load(p + 1) : p[1];
+            return;
+        }
+        clear();
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (c + j < d) raw[j / 4][j % 4] = row[c + j];
+    }
+    __device__ __forceinline__ void clear() { raw[0] = raw[1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f}; }
+    __device__ __forceinline__ void values(int64_t, int64_t, float (&f)[8]) const {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = raw[j / 4][j % 4];
+    }
+};
+template <bool STREAM>
+__device__ __forceinline__ void store_values(uint16_t* row, int64_t c, int64_t d, const float (&f)[8]) { store8<STREAM>(row, c, d, narrow8(f)); }
+template <bool STREAM>
+__device__ __forceinline__ void store_values(float* row, int64_t c, int64_t d, const float (&f)[8]) {
+    f32x4_anywhere* p = reinterpret_cast<f32x4_anywhere*>(row + c);
+    const f32x4 low = {f[0], f[1], f[2], f[3]}, high = {f[4], f[5], f[6], f[7]};
+    if (c + 8 <= d) {
+        if (STREAM) { __builtin_nontemporal_store(low, p); __builtin_nontemporal_store(high, p + 1); }
+        else { p[0] = low; p[1] = high; }
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (c + j < d) row[c + j] = f[j];
+}
+
 // One wave per token and span: a sum over the token's choices in binary32, in their order, so no atomics.  Bound by the rows read (two of
-// 4096 for each of 8192 tokens: 33 us, 6.1 TB/s).  The rows are BF16, as a product writes them: a rounding more (2^-9 of each row's
-// elements, where their 4-bit factors carry 2^-3), for half of the bytes that product and sum move.
-template <bool WEIGHTS, bool STREAM>
-__global__ __launch_bounds__(256) void k_expert_combine(const uint16_t* ys, int64_t ld_ys, int64_t d, MxOrder o, const float* weights,
-                                                        uint16_t* y, int64_t ld_y, uint32_t spans) {
+// 4096 for each of 8192 tokens: 33 us, 6.1 TB/s).  Rows are BF16 or binary32, as a product writes them: BF16 is a rounding more (2^-9 of
+// each row's elements, where their 4-bit factors carry 2^-3) for half of the bytes that product and sum move.
+template <class IN, class OUT, bool WEIGHTS, bool STREAM>
+__global__ __launch_bounds__(256) void k_expert_combine(const IN* ys, int64_t ld_ys, int64_t d, MxOrder o, const float* weights,
+                                                        OUT* y, int64_t ld_y, uint32_t spans) {
     const uint32_t group = blockIdx.x / spans, span = blockIdx.x - group * spans;
     const int64_t token = (int64_t)group * 4 + (threadIdx.x >> 6);
     if (token >= o.tokens) return;
@@ -183,7 +233,7 @@ __global__ __launch_bounds__(256) void k_expert_combine(const uint16_t* ys, int6
     for (int j0 = 0; j0 < o.top_k; j0 += kAtOnce) {
         uint32_t slot[kAtOnce];
         float w[kAtOnce];
-        u32x4 rows[kAtOnce][2];
+        Piece<IN, STREAM> rows[kAtOnce][2];
 #pragma unroll
         for (int j = 0; j < kAtOnce; ++j) {
             const int64_t choice = token * o.top_k + j0 + j;
@@ -195,7 +245,8 @@ __global__ __launch_bounds__(256) void k_expert_combine(const uint16_t* ys, int6
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int64_t c = (int64_t)span * kRowSpan + h * 512 + (threadIdx.x & 63) * 8;
-                rows[j][h] = slot[j] < (uint32_t)o.capacity && c < d ? load8_start<STREAM>(ys + slot[j] * ld_ys, c, d) : u32x4{0u, 0u, 0u, 0u};
+                if (slot[j] < (uint32_t)o.capacity && c < d) rows[j][h].load(ys + slot[j] * ld_ys, c, d);
+                else rows[j][h].clear();
             }
 #pragma unroll
         for (int j = 0; j < kAtOnce; ++j) {
@@ -204,7 +255,7 @@ __global__ __launch_bounds__(256) void k_expert_combine(const uint16_t* ys, int6
             for (int h = 0; h < 2; ++h) {
                 const int64_t c = (int64_t)span * kRowSpan + h * 512 + (threadIdx.x & 63) * 8;
                 float f[8];
-                widen8(c < d ? load8_end(rows[j][h], c, d) : rows[j][h], f);
+                rows[j][h].values(c, d, f);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) acc[h][i] += WEIGHTS ? w[j] * f[i] : f[i];
             }
@@ -213,14 +264,14 @@ __global__ __launch_bounds__(256) void k_expert_combine(const uint16_t* ys, int6
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const int64_t c = (int64_t)span * kRowSpan + h * 512 + (threadIdx.x & 63) * 8;
-        if (c < d) store8<STREAM>(y + token * ld_y, c, d, narrow8(acc[h]));
+        if (c < d) store_values<STREAM>(y + token * ld_y, c, d, acc[h]);
     }
 }
 
 // One wave per slot: the token's row is read for both gradients.  The lanes' partial sums, in binary32, are joined in a fixed order.
 // Bound by memory (16384 of 18432 slots of 4096, both gradients: 65 us, 5.4 TB/s; of 2048, the weights' alone: 21 us, 4.8 TB/s).
-template <bool DYS, bool DW, bool STREAM>
-__global__ __launch_bounds__(256) void k_expert_combine_backward(const uint16_t* dy, int64_t ld_dy, const uint16_t* ys, int64_t ld_ys, int64_t d,
+template <class IN, bool DYS, bool DW, bool STREAM>
+__global__ __launch_bounds__(256) void k_expert_combine_backward(const uint16_t* dy, int64_t ld_dy, const IN* ys, int64_t ld_ys, int64_t d,
                                                                  MxOrder o, const float* weights, uint16_t* dys, int64_t ld_dys, float* dweights) {
     const int64_t choices = (int64_t)o.tokens * o.top_k;
     if (DW) {                           // dropped choices have no slot: their zeros are shared out over all lanes
@@ -239,8 +290,10 @@ __global__ __launch_bounds__(256) void k_expert_combine_backward(const uint16_t*
         float g[8] = {};
         if (used) widen8(load8(row, c, d), g);
         if (DW && used) {
+            Piece<IN, STREAM> piece;
+            piece.load(ys + slot * ld_ys, c, d);
             float f[8];
-            widen8(load8<STREAM>(ys + slot * ld_ys, c, d), f);
+            piece.values(c, d, f);
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum = __builtin_fmaf(g[i], f[i], sum);
         }
@@ -300,36 +353,59 @@ hipError_t launch_expert_gather(const uint16_t* x, int64_t ld_x, int64_t d, cons
     return hipGetLastError();
 }
 
-hipError_t launch_expert_combine(const uint16_t* ys, int64_t ld_ys, int64_t d, const MxOrder& o, const float* weights, uint16_t* y,
-                                 int64_t ld_y, hipStream_t st) {
+// (in elements of two bytes)
+static bool streamed(int64_t elements, const uint16_t* rows, int64_t ld) { return mx_streamed(elements, rows, ld, 0); }
+static bool streamed(int64_t elements, const float* rows, int64_t ld) { return mx_streamed(elements * 2, reinterpret_cast<const uint16_t*>(rows), ld * 2, 0); }
+
+template <class IN, class OUT>
+static hipError_t combine(const IN* ys, int64_t ld_ys, int64_t d, const MxOrder& o, const float* weights, OUT* y, int64_t ld_y, hipStream_t st) {
     const uint32_t spans = row_spans(d);
     const int64_t blocks = (int64_t)four_per_block(o.tokens) * spans;
     if (blocks > 0x7FFFFFFFll) return hipErrorInvalidValue;
     const dim3 grid((uint32_t)blocks);
-    const bool stream = mx_streamed(o.capacity * d, ys, ld_ys, 0) && mx_streamed(o.capacity * d, y, ld_y, 0);
+    const bool stream = streamed(o.capacity * d, ys, ld_ys) && streamed(o.capacity * d, y, ld_y);
     if (weights) {
-        if (stream) k_expert_combine<true, true><<<grid, dim3(256), 0, st>>>(ys, ld_ys, d, o, weights, y, ld_y, spans);
-        else k_expert_combine<true, false><<<grid, dim3(256), 0, st>>>(ys, ld_ys, d, o, weights, y, ld_y, spans);
+        if (stream) k_expert_combine<IN, OUT, true, true><<<grid, dim3(256), 0, st>>>(ys, ld_ys, d, o, weights, y, ld_y, spans);
+        else k_expert_combine<IN, OUT, true, false><<<grid, dim3(256), 0, st>>>(ys, ld_ys, d, o, weights, y, ld_y, spans);
     } else {
-        if (stream) k_expert_combine<false, true><<<grid, dim3(256), 0, st>>>(ys, ld_ys, d, o, weights, y, ld_y, spans);
-        else k_expert_combine<false, false><<<grid, dim3(256), 0, st>>>(ys, ld_ys, d, o, weights, y, ld_y, spans);
+        if (stream) k_expert_combine<IN, OUT, false, true><<<grid, dim3(256), 0, st>>>(ys, ld_ys, d, o, weights, y, ld_y, spans);
+        else k_expert_combine<IN, OUT, false, false><<<grid, dim3(256), 0, st>>>(ys, ld_ys, d, o, weights, y, ld_y, spans);
     }
     return hipGetLastError();
 }
+hipError_t launch_expert_combine(const uint16_t* ys, int64_t ld_ys, int64_t d, const MxOrder& o, const float* weights, uint16_t* y,
+                                 int64_t ld_y, hipStream_t st) {
+    return combine(ys, ld_ys, d, o, weights, y, ld_y, st);
+}
+hipError_t launch_expert_combine_f32(const float* ys, int64_t ld_ys, int64_t d, const MxOrder& o, const float* weights, void* y, int64_t ld_y,
+                                     bool y_f32, hipStream_t st) {
+    return y_f32 ? combine(ys, ld_ys, d, o, weights, static_cast<float*>(y), ld_y, st) : combine(ys, ld_ys, d, o, weights, static_cast<uint16_t*>(y), ld_y, st);
+}
 
-template <bool STREAM>
-static void combine_backward(const uint16_t* dy, int64_t ld_dy, const uint16_t* ys, int64_t ld_ys, int64_t d, const MxOrder& o,
+template <class IN, bool STREAM>
+static void combine_backward(const uint16_t* dy, int64_t ld_dy, const IN* ys, int64_t ld_ys, int64_t d, const MxOrder& o,
                              const float* weights, uint16_t* dys, int64_t ld_dys, float* dweights, hipStream_t st) {
     const dim3 grid(four_per_block(o.capacity));
-    if (dys && dweights) k_expert_combine_backward<true, true, STREAM><<<grid, dim3(256), 0, st>>>(dy, ld_dy, ys, ld_ys, d, o, weights, dys, ld_dys, dweights);
-    else if (dys) k_expert_combine_backward<true, false, STREAM><<<grid, dim3(256), 0, st>>>(dy, ld_dy, ys, ld_ys, d, o, weights, dys, ld_dys, dweights);
-    else k_expert_combine_backward<false, true, STREAM><<<grid, dim3(256), 0, st>>>(dy, ld_dy, ys, ld_ys, d, o, weights, dys, ld_dys, dweights);
+    if (dys && dweights) k_expert_combine_backward<IN, true, true, STREAM><<<grid, dim3(256), 0, st>>>(dy, ld_dy, ys, ld_ys, d, o, weights, dys, ld_dys, dweights);
+    else if (dweights) k_expert_combine_backward<IN, false, true, STREAM><<<grid, dim3(256), 0, st>>>(dy, ld_dy, ys, ld_ys, d, o, weights, dys, ld_dys, dweights);
+    else                                // reads no rows, of whatever type
+        k_expert_combine_backward<uint16_t, true, false, STREAM><<<grid, dim3(256), 0, st>>>(dy, ld_dy, nullptr, 0, d, o, weights, dys, ld_dys, dweights);
+}
+template <class IN>
+static hipError_t backward(const uint16_t* dy, int64_t ld_dy, const IN* ys, int64_t ld_ys, int64_t d, const MxOrder& o, const float* weights,
+                           uint16_t* dys, int64_t ld_dys, float* dweights, hipStream_t st) {
+    if ((!ys || streamed(o.capacity * d, ys, ld_ys)) && (!dys || streamed(o.capacity * d, dys, ld_dys)))
+        combine_backward<IN, true>(dy, ld_dy, ys, ld_ys, d, o, weights, dys, ld_dys, dweights, st);
+    else combine_backward<IN, false>(dy, ld_dy, ys, ld_ys, d, o, weights, dys, ld_dys, dweights, st);
+    return hipGetLastError();
 }
 hipError_t launch_expert_combine_backward(const uint16_t* dy, int64_t ld_dy, const uint16_t* ys, int64_t ld_ys, int64_t d, const MxOrder& o,
                                           const float* weights, uint16_t* dys, int64_t ld_dys, float* dweights, hipStream_t st) {
-    if ((!ys || mx_streamed(o.capacity * d, ys, ld_ys, 0)) && (!dys || mx_streamed(o.capacity * d, dys, ld_dys, 0))) combine_backward<true>(dy, ld_dy, ys, ld_ys, d, o, weights, dys, ld_dys, dweights, st);
-    else combine_backward<false>(dy, ld_dy, ys, ld_ys, d, o, weights, dys, ld_dys, dweights, st);
-    return hipGetLastError();
+    return backward(dy, ld_dy, ys, ld_ys, d, o, weights, dys, ld_dys, dweights, st);
+}
+hipError_t launch_expert_combine_backward_f32(const uint16_t* dy, int64_t ld_dy, const float* ys, int64_t ld_ys, int64_t d, const MxOrder& o,
+                                              const float* weights, uint16_t* dys, int64_t ld_dys, float* dweights, hipStream_t st) {
+    return backward(dy, ld_dy, ys, ld_ys, d, o, weights, dys, ld_dys, dweights, st);
 }
 
 }  // namespace mor

@@ -76,7 +76,11 @@ hipError_t launch_expert_sort(const int32_t* ids, const MxOrder& o, void* worksp
 hipError_t launch_expert_gather(const uint16_t* x, int64_t ld_x, int64_t d, const MxOrder& o, uint16_t* xs, int64_t ld_xs, hipStream_t st);
 hipError_t launch_expert_combine(const uint16_t* ys, int64_t ld_ys, int64_t d, const MxOrder& o, const float* weights, uint16_t* y,
                                  int64_t ld_y, hipStream_t st);
+hipError_t launch_expert_combine_f32(const float* ys, int64_t ld_ys, int64_t d, const MxOrder& o, const float* weights, void* y, int64_t ld_y,
+                                     bool y_f32, hipStream_t st);
 hipError_t launch_expert_combine_backward(const uint16_t* dy, int64_t ld_dy, const uint16_t* ys, int64_t ld_ys, int64_t d, const MxOrder& o,
                                           const float* weights, uint16_t* dys, int64_t ld_dys, float* dweights, hipStream_t st);
+hipError_t launch_expert_combine_backward_f32(const uint16_t* dy, int64_t ld_dy, const float* ys, int64_t ld_ys, int64_t d, const MxOrder& o,
+                                              const float* weights, uint16_t* dys, int64_t ld_dys, float* dweights, hipStream_t st);
 
 }  // namespace mor

@@ -21,7 +21,7 @@ EXPERTS_MAX = 1024
 
 EXPORTS = ("mor_mx_quantize", "mor_mx_dequantize", "mor_mx_product_workspace_bytes", "mor_mx_product", "mor_mx_product_rows",
            "mor_mx_product_depth", "mor_expert_capacity", "mor_expert_workspace_bytes", "mor_expert_sort", "mor_expert_gather",
-           "mor_expert_combine", "mor_expert_combine_backward")
+           "mor_expert_combine", "mor_expert_combine_f32", "mor_expert_combine_backward", "mor_expert_combine_backward_f32")
 
 
 class MorMxOperand(C.Structure):
@@ -62,6 +62,8 @@ def load():
             "mor_expert_sort": ([ptr, order, ptr, C.c_size_t, ptr], C.c_int),
             "mor_expert_gather": ([ptr, i64, i64, order, ptr, i64, ptr], C.c_int),
             "mor_expert_combine": ([ptr, i64, i64, order, ptr, ptr, i64, ptr], C.c_int),
+            "mor_expert_combine_f32": ([ptr, i64, i64, order, ptr, ptr, i64, C.c_int32, ptr], C.c_int),
+            "mor_expert_combine_backward_f32": ([ptr, i64, ptr, i64, i64, order, ptr, ptr, i64, ptr, ptr], C.c_int),
             "mor_expert_combine_backward": ([ptr, i64, ptr, i64, i64, order, ptr, ptr, i64, ptr, ptr], C.c_int),
         }
         for name, (args, result) in signatures.items():
@@ -307,10 +309,10 @@ def mor_expert_sort(ids: torch.Tensor, order: ExpertOrder) -> None:
          ws.numel() if ws is not None else 0)
 
 
-def _rows(t: torch.Tensor | None, name: str, rows: int, d: int) -> int:
+def _rows(t: torch.Tensor | None, name: str, rows: int, d: int, types=(torch.bfloat16, torch.int16)) -> int:
     if t is None:
         return 0
-    ld = _matrix(t, name)
+    ld = _matrix(t, name, types)
     if t.shape != (rows, d):
         raise ValueError(f"{name} must be {rows} x {d}, not {tuple(t.shape)}")
     return ld
@@ -326,24 +328,31 @@ def mor_expert_gather(x: torch.Tensor, order: ExpertOrder, xs: torch.Tensor) -> 
     _run("mor_expert_gather", device, x.data_ptr(), ld_x, d, order.struct(), xs.data_ptr(), ld_xs)
 
 
+_ROWS = (torch.bfloat16, torch.int16, torch.float32)
+
+
 def mor_expert_combine(ys: torch.Tensor, order: ExpertOrder, weights: torch.Tensor | None, y: torch.Tensor) -> None:
-    """``y`` (tokens, d): weighted sum of each token's rows of ``ys`` (capacity, d)."""
+    """``y`` (tokens, d): weighted sum of each token's rows of ``ys`` (capacity, d).  BF16, or rows in float32 and ``y`` in either."""
     d = ys.shape[-1]
-    ld_ys, ld_y = _rows(ys, "ys", order.capacity, d), _rows(y, "y", order.tokens, d)
+    f32 = ys.dtype == torch.float32
+    ld_ys, ld_y = _rows(ys, "ys", order.capacity, d, _ROWS), _rows(y, "y", order.tokens, d, _ROWS if f32 else _ROWS[:2])
     _vector(weights, "weights", torch.float32, order.tokens * order.top_k)
+    where = "mor_expert_combine_f32" if f32 else "mor_expert_combine"
     device = order._index
     if ys.get_device() != device or y.get_device() != device or (weights is not None and weights.get_device() != device):
-        _device("mor_expert_combine", ys, order, weights, y)
-    _run("mor_expert_combine", device, ys.data_ptr(), ld_ys, d, order.struct(), binding._ptr(weights), y.data_ptr(), ld_y)
+        _device(where, ys, order, weights, y)
+    _run(where, device, ys.data_ptr(), ld_ys, d, order.struct(), binding._ptr(weights), y.data_ptr(), ld_y,
+         *((int(y.dtype == torch.float32),) if f32 else ()))
 
 
 def mor_expert_combine_backward(dy: torch.Tensor, ys: torch.Tensor | None, order: ExpertOrder, weights: torch.Tensor | None,
                                 dys: torch.Tensor | None, dweights: torch.Tensor | None) -> None:
-    """Gradients of :func:`mor_expert_combine`: ``dys`` (capacity, d) and ``dweights`` (tokens, top_k), either may be None."""
+    """Gradients of :func:`mor_expert_combine`: ``dys`` (capacity, d; BF16) and ``dweights`` (tokens, top_k), either may be None."""
     d = dy.shape[-1]
-    ld_dy, ld_ys, ld_dys = _rows(dy, "dy", order.tokens, d), _rows(ys, "ys", order.capacity, d), _rows(dys, "dys", order.capacity, d)
+    ld_dy, ld_ys, ld_dys = _rows(dy, "dy", order.tokens, d), _rows(ys, "ys", order.capacity, d, _ROWS), _rows(dys, "dys", order.capacity, d)
     _vector(weights, "weights", torch.float32, order.tokens * order.top_k)
     _vector(dweights, "dweights", torch.float32, order.tokens * order.top_k)
-    device = _device("mor_expert_combine_backward", dy, ys, order, weights, dys, dweights)
-    _run("mor_expert_combine_backward", device, dy.data_ptr(), ld_dy, binding._ptr(ys), ld_ys, d, order.struct(), binding._ptr(weights),
-         binding._ptr(dys), ld_dys, binding._ptr(dweights))
+    where = "mor_expert_combine_backward_f32" if ys is not None and ys.dtype == torch.float32 else "mor_expert_combine_backward"
+    device = _device(where, dy, ys, order, weights, dys, dweights)
+    _run(where, device, dy.data_ptr(), ld_dy, binding._ptr(ys), ld_ys, d, order.struct(),
+         binding._ptr(weights), binding._ptr(dys), ld_dys, binding._ptr(dweights))

@@ -17,6 +17,8 @@ from . import mx
 
 
 def _bf16(t: torch.Tensor) -> torch.Tensor:
+    """What is quantised.  Float32 values are rounded to BF16 before they are rounded to four bits, by a pass of torch's: off by 2^-9 of
+    themselves before a step of 2^-3."""
     t = t.detach().to(torch.bfloat16)
     return t if t.stride(-1) == 1 and t.stride(-2) >= t.shape[-1] else t.contiguous()
 
@@ -136,6 +138,12 @@ def linear(x: torch.Tensor, w: torch.Tensor, scale_rule: str = "floor", seed: in
     return _Linear.apply(x, w, scale_rule, how, training)
 
 
+def _row_type(x: torch.Tensor) -> torch.dtype:
+    """Of the experts' rows between the product and the sum over a token's choices, and of the tokens' gradient: BF16 where the tokens are,
+    one rounding more for half of the bytes; float32, without it, where those are float32."""
+    return torch.float32 if x.dtype == torch.float32 else torch.bfloat16
+
+
 class _Experts(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, w, ids, weights, scale_rule, how, training):
@@ -146,7 +154,7 @@ class _Experts(torch.autograd.Function):
         mx.mor_expert_sort(ids, order)
         xq, xt = _operands(_bf16(x), order.capacity, hidden, training and ctx.needs_input_grad[1], scale_rule=scale_rule, order=order)
         wq, wt = _operands(_bf16(w), width, hidden, training and ctx.needs_input_grad[0], experts, scale_rule=scale_rule)
-        ys = torch.empty(order.capacity, width, dtype=torch.bfloat16, device=x.device)
+        ys = torch.empty(order.capacity, width, dtype=_row_type(x), device=x.device)
         mx.mor_mx_product_rows(xq, wq, order, ys)
         y = torch.empty(tokens, width, dtype=torch.bfloat16, device=x.device)
         weights = weights.detach().contiguous()
@@ -169,11 +177,10 @@ class _Experts(torch.autograd.Function):
             # the rows' gradients, each times its choice's weight, go from the tokens' straight into 4 bits
             g, gt = _operands(dy, order.capacity, dy.shape[1], xt is not None, plain=wt is not None, order=order, weights=weights, **ctx.how)
         if wt is not None:
-            dxs = torch.empty(order.capacity, wt.rows, dtype=torch.bfloat16, device=dy.device)
+            dxs = torch.empty(order.capacity, wt.rows, dtype=ctx.types[0], device=dy.device)
             mx.mor_mx_product_rows(g, wt, order, dxs)
-            dx = torch.empty(order.tokens, wt.rows, dtype=torch.bfloat16, device=dy.device)
+            dx = torch.empty(order.tokens, wt.rows, dtype=ctx.types[0], device=dy.device)
             mx.mor_expert_combine(dxs, order, None, dx)
-            dx = dx.to(ctx.types[0])
         if xt is not None:
             dw = torch.empty(order.n_experts, dy.shape[1], xt.rows, dtype=ctx.types[1], device=dy.device)
             mx.mor_mx_product_depth(gt, xt, order, dw)
@@ -186,8 +193,9 @@ class _Experts(torch.autograd.Function):
 def experts(x: torch.Tensor, w: torch.Tensor, ids: torch.Tensor, weights: torch.Tensor, scale_rule: str = "floor",
             seed: int | None = None, gradient_rule: str | None = None) -> torch.Tensor:
     """Sum over a token's choices ``ids`` (tokens, top_k; int32, outside the experts: dropped) of its ``weights`` (tokens, top_k; float32) times
-    the token's row of ``x`` (tokens, hidden) times that expert's matrix of ``w`` (experts, width, hidden), transposed; in BF16.  ``seed``
-    and ``gradient_rule`` as for :func:`linear`."""
+    the token's row of ``x`` (tokens, hidden) times that expert's matrix of ``w`` (experts, width, hidden), transposed; in BF16.  Float32
+    tokens keep the experts' rows in float32 until they are added up, and get a float32 gradient.  ``seed`` and
+    ``gradient_rule`` as for :func:`linear`."""
     _check(x, w, 3)
     _check_choices(x, ids, weights)
     training = torch.is_grad_enabled()
@@ -212,7 +220,7 @@ class ServedExperts:
         order = mx.alloc_order(tokens, ids.shape[1], self.w.batch, x.device, align=1)
         mx.mor_expert_sort(ids.contiguous(), order)
         xq, _ = _operands(_bf16(x), order.capacity, hidden, False, scale_rule=self.scale_rule, order=order)
-        ys = torch.empty(order.capacity, self.w.rows, dtype=torch.bfloat16, device=x.device)
+        ys = torch.empty(order.capacity, self.w.rows, dtype=_row_type(x), device=x.device)
         mx.mor_mx_product_rows(xq, self.w, order, ys)
         y = torch.empty(tokens, self.w.rows, dtype=torch.bfloat16, device=x.device)
         mx.mor_expert_combine(ys, order, weights.contiguous(), y)

@@ -156,3 +156,52 @@ def test_forms_that_nothing_reads_are_not_made(kind, monkeypatch):
                 made.clear()
                 y.backward(dy)
             assert made == ([(need_x, need_w)] if need_x or need_w else [])
+
+
+def test_experts_of_binary32_tokens_keep_binary32_rows():
+    """Rows between product and sum, the tokens' gradient and the routing weights' gradient without a rounding to BF16: each element is within
+    the products' bounds, the sums' (top_k + 1) 2^-24 or d 2^-24, and one rounding to the type of the result.  Routing weights of both
+    signs, so that rows cancel."""
+    tokens, top_k, experts, hidden, width = 150, 3, 4, 130, 64
+    x, w, ids, weights, dy = layer(tokens, top_k, experts, hidden, width, seed=7)
+    weights = np.where(np.arange(top_k) % 2, -weights, weights).astype(np.float32)
+    xg, wg = (t.to(DEV, torch.float32).requires_grad_() for t in (x, w))
+    weights_g = torch.from_numpy(weights).to(DEV).requires_grad_()
+    y = mx_layers.experts(xg, wg, torch.from_numpy(ids).to(DEV), weights_g, seed=9)
+    y.backward(dy.to(DEV))
+    served = mx_layers.ServedExperts(w.to(DEV))(x.to(DEV, torch.float32), torch.from_numpy(ids).to(DEV), torch.from_numpy(weights).to(DEV))
+
+    capacity = mx.expert_capacity(tokens, top_k, experts)
+    starts, slot, src = R.sort(ids, experts, 128, capacity)
+    used = src >= 0
+    rows, grads = np.zeros((capacity, hidden)), np.zeros((capacity, width))
+    rows[used] = numbers(x)[src[used] // top_k]
+    grads[used] = (numbers(dy).astype(np.float32)[src[used] // top_k] * weights.reshape(-1)[src[used], None]).astype(np.float64)
+    xq, g = forms(rows, "floor")[0], forms(grads, "floor", 9)[0]
+    ys, ys_off, dxs, dxs_off = (np.zeros((capacity, n)) for n in (width, width, hidden, hidden))
+    for e in range(experts):
+        s = slice(starts[e], starts[e + 1])
+        wq, wt = forms(numbers(w[e]), "floor")
+        ys[s], ys_off[s] = xq[s] @ wq.T, sums_bound(xq[s], wq)
+        dxs[s], dxs_off[s] = g[s] @ wt, sums_bound(g[s], wt.T)
+    ys_off += 2.0 ** -24 * np.abs(ys)
+    dxs_off += 2.0 ** -24 * np.abs(dxs)
+
+    def added_up(of, off, factor):
+        total, bound = np.zeros((tokens, of.shape[1])), np.zeros((tokens, of.shape[1]))
+        for i, at in enumerate(slot):
+            if at >= 0:
+                total[i // top_k] += factor[i] * of[at]
+                bound[i // top_k] += abs(factor[i]) * (off[at] + (top_k + 1) * 2.0 ** -24 * np.abs(of[at]))
+        return total, bound
+
+    for got in (y, served):
+        check(got, *added_up(ys, ys_off, weights.reshape(-1).astype(np.float64)))
+    check(xg.grad, *added_up(dxs, dxs_off, np.ones(tokens * top_k)), True)
+    dots, dots_off = np.zeros(tokens * top_k), np.zeros(tokens * top_k)
+    for i, at in enumerate(slot):
+        if at >= 0:
+            d = np.abs(numbers(dy)[i // top_k])
+            dots[i] = numbers(dy)[i // top_k] @ ys[at]
+            dots_off[i] = d @ ys_off[at] + (width + 1) * 2.0 ** -24 * (d @ np.abs(ys[at]))
+    check(weights_g.grad, dots.reshape(tokens, top_k), dots_off.reshape(tokens, top_k), True)
