@@ -947,6 +947,7 @@ static hipError_t launch_few(int mode, const MxProductArgs& p, hipStream_t st) {
     const dim3 grid((uint32_t)(n_tiles * m_tiles)), block(kFewWaves * 64);
     if (mode == kMxDense) k_mx_few<kMxDense, MT, NT><<<grid, block, 0, st>>>(p, (uint32_t)n_tiles);
     else if constexpr (MT == 4 || (MT == 1 && NT <= 2)) k_mx_few<kMxRows, MT, NT><<<grid, block, 0, st>>>(p, (uint32_t)n_tiles);
+    else return hipErrorInvalidValue;                   // no kernel of this shape: plan_product asks for none
     return hipGetLastError();
 }
 
