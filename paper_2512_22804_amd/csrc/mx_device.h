@@ -23,9 +23,6 @@ __device__ __forceinline__ uint32_t mx_scale_byte(uint32_t amax_bits, bool ceil_
     if (ceil_rule && (amax_bits & 0x7FFFFFu) > 0x400000u) ++e;      // amax > 1.5 * 2^(e+2) = 6 * 2^e
     return (uint32_t)max(e, 0);
 }
-// 2^(byte - 127) and its inverse as binary32; byte 0 is the subnormal 2^-127.
-__device__ __forceinline__ float mx_scale_value(uint32_t byte) { return __uint_as_float(byte ? byte << 23 : 0x00400000u); }
-__device__ __forceinline__ float mx_scale_inverse(uint32_t byte) { return __uint_as_float((254u - min(byte, 253u)) << 23); }
 
 // Philox 4 x 32 (J. Salmon, M. Moraes, R. Dror, D. Shaw: "Parallel random numbers: as easy as 1, 2, 3", 2011) with seven
 // rounds, the fewest for which the authors report that every statistical test passes; ten cost 1.4 times as much.
@@ -108,7 +105,6 @@ __device__ __forceinline__ void widen8(const u32x4& raw, float (&v)[8]) {
         v[2 * j + 1] = __uint_as_float(raw[j] & 0xFFFF0000u);
     }
 }
-
 
 // The XCDs take the workgroups in turn: tile of workgroup `b` of `n`, such that each XCD has a run of neighbouring ones.  Lines that two
 // tiles share then meet in one L2, whole when they leave it (de-quantisation of 14336 x 4096: 27.7 us in the workgroups' own order,
