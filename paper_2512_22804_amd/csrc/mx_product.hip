@@ -871,8 +871,10 @@ static double tile_rows(int mode, const MxProductArgs& p, int height) {
 static ProductPlan plan_product(int mode, const MxProductArgs& p) {
     const int64_t m = p.m, n = p.n, blocks = p.blocks;
     // (More than 32 rows and a long depth for few workgroups: parts of the depth are better.  64 x 4096 x 14336: 22.5 us, 18.8 in tiles;
-    // 64 x 4096 x 8192: 15.3 and 17.3.)  Up to four rows are read often at little cost (1 x 14336 x 4096 with 16, 32 and 64 rows of
-    // B: 8.9, 9.6, 9.6).
+    // 64 x 4096 x 8192: 15.3 and 17.3.)  Up to four rows are read often at little cost, so that more
+    // workgroups are worth it (with 16 rows of B and by few_nt, 1, 2 and 4 rows, n from 5200 to 20000, k from 512 to 8192: up to 20 %
+    // less, 1 x 20000 x 8192 21.8 and 26.2 us, 1 x 8192 x 4096 5.8 and 6.2, 4 x 14336 x 512 3.8 and 4.6; at the worst 8 % more,
+    // 4 x 14336 x 4096 9.4 and 8.5 to 9.3, 4 x 5200 x 8192 9.7 and 9.0).
     if (mode == kMxDense && m <= 64 && !(m > 32 && n < 160 * 32 && blocks > 320))
         return {ProductPlan::kFew, 1, m <= 16 ? 1 : m <= 32 ? 2 : 4, m <= 4 && n < 160 * 128 ? 1 : few_nt((double)n)};
     // Rows of experts: every expert's matrix is read once in tiles, once for each 16 of its rows otherwise.  (Experts of 2048 x 4096, us
