@@ -3,6 +3,7 @@ refused instead of lost, operands kept where autograd sees them, no work that no
 import numpy as np
 import pytest
 import torch
+import torch.utils.checkpoint
 
 import mx_refmodel as R
 from paper_2512_22804_amd import mx, mx_layers
@@ -133,6 +134,26 @@ def test_kept_operands_are_saved_tensors(kind):
     assert torch.equal(a.grad, 2 * want[0]) and torch.equal(b.grad, 2 * want[1])
     with pytest.raises(RuntimeError):
         y.backward(dy)
+
+
+@pytest.mark.parametrize("reentrant", [False, True])
+@pytest.mark.parametrize("kind", ["linear", "experts"])
+def test_checkpointing(kind, reentrant):
+    x, w, args, dy, *_ = case(kind)
+    torch.manual_seed(6)
+    want = gradients(kind, dy, x, w, args)
+    torch.manual_seed(6)
+    a, b = x.clone().requires_grad_(), w.clone().requires_grad_()
+    torch.utils.checkpoint.checkpoint(lambda a, b: answer(kind, a, b, args), a, b, use_reentrant=reentrant).backward(dy)
+    assert torch.equal(a.grad, want[0]) and torch.equal(b.grad, want[1])
+
+
+@pytest.mark.parametrize("kind", ["linear", "experts"])
+def test_inference_mode(kind):
+    x, w, args, *_ = case(kind)
+    want = answer(kind, x, w, args)
+    with torch.inference_mode():
+        assert torch.equal(answer(kind, x.clone().requires_grad_(), w, args), want)
 
 
 @pytest.mark.parametrize("kind", ["linear", "experts"])
