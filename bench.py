@@ -43,13 +43,14 @@ def log(*a):
 
 
 def csrc_sha256() -> str:
-    """Hash of the kernel sources and the public header of this tree (what a rocprofv3 traffic measurement is tied to)."""
+    """Hash of the sources of this benchmark's kernels and of their public header (what a rocprofv3 traffic measurement is tied to).  The
+    4-bit operators (mx_*) are launched nowhere here and included by none of the others."""
     import hashlib
     h = hashlib.sha256()
     base = os.path.join(ROOT, "paper_2512_22804_amd", "csrc")
     for f in sorted(os.listdir(base)) + [os.path.join("..", "..", "include", "mor.h")]:
         path = os.path.join(base, f)
-        if os.path.isfile(path) and not f.endswith((".o", ".so")):
+        if os.path.isfile(path) and not f.startswith("mx_") and not f.endswith((".o", ".so")):
             h.update(os.path.basename(f).encode() + b"\0" + open(path, "rb").read())
     return h.hexdigest()[:16]
 
