@@ -204,10 +204,11 @@ __global__ __launch_bounds__(64) void k_mx_product(MxProductArgs p, uint32_t n_t
 // address out of range in the last stage, and stages beyond the last, whose range is empty.  The scale bytes behind the last
 // block, loaded 16 at a time, are replaced by 2^0: whatever they hold, a NaN too, counts for nothing.
 //
-// 8192 x 14336 x 4096: 241 us, 4.0 PFLOP/s.  The same instructions on random operands that stay in registers reach 6.6 at 1.7 GHz, the
-// clock that the power allows, and 9.6 on zeros; without the requests the loop would take a seventh less, and a tile's way out
-// (its sums through LDS to memory, at about 8 us of 35) is not covered by the next one's products, since the sums and
-// their successors do not both fit into the registers.
+// 8192 x 14336 x 4096: 241 to 258 us on several cards, 3.7 to 4.0 PFLOP/s.  The same instructions on random operands that stay in registers
+// reach 6.4 at 1.65 GHz, the clock that the power allows, and 9.6 on zeros.  Here the matrix instructions are busy for 49 % of the
+// cycles and LDS for 20 %.  A tile's way out (its sums through LDS to memory, about 8 us of 35) is not covered by the next one's
+// products, since the sums and their successors do not both fit into the registers; the rest goes in the stages, between the
+// matrix instructions.
 
 constexpr uint32_t kNowhere = 0x7FFFFFFFu;              // an offset that no range contains
 

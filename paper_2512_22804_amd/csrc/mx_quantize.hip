@@ -19,7 +19,7 @@ constexpr int kTileCols = 128;          // columns of a workgroup's tile: 16 lan
 // by the vector unit (40, 40 and 63 us): a generator's seven rounds for eight elements and a dozen instructions for each.  Both forms
 // in one launch read the tensor once, and a lane's eight rows are in flight together; tiles half as wide, twice as many on a
 // CU, were slower (48 us for both).  Weighted rows are scaled in binary32 and not rounded in between (18432 x 2048 gathered, both
-// forms, stochastic: 54 us).
+// forms, stochastic: 60 us: a slot, its choice's weight and its token's row are loads that wait for each other).
 template <int RPT, bool ROWS, bool T, bool SR, bool WEIGHTED, bool STREAM>
 __global__ __launch_bounds__(256, T && WEIGHTED ? 3 : 1) void k_mx_quantize(MxQuantArgs a, uint32_t col_tiles) {
     static_assert(!T || RPT == 8 || RPT == 2, "the transposed form works on tiles of 128 or 32 rows");
@@ -167,8 +167,8 @@ __global__ __launch_bounds__(256, T && WEIGHTED ? 3 : 1) void k_mx_quantize(MxQu
 
 // The rows form of tokens sorted by expert, rounded to nearest and without weights: every slot of a token holds the same codes.  So a
 // token's row is read and quantised once and written to its choices' slots, and further workgroups, 32 slots each, fill the empty
-// ones with zeros.  (8192 x 4096 into two slots each: 19 us = 5.4 TB/s of what is read and written once; slot by slot, every row read
-// and quantised twice, 30 us.)
+// ones with zeros.  (8192 x 4096 into two slots each: 19 us = 5.4 TB/s of what is read and written once, 27 us on tokens that no
+// cache holds; slot by slot, every row read and quantised twice, 30 us.)
 constexpr int kFillSlots = 32;
 template <int RPT>
 __global__ __launch_bounds__(256) void k_mx_quantize_tokens(MxQuantArgs a, uint32_t col_tiles, uint32_t token_groups) {
